@@ -100,7 +100,7 @@ enum {
   NSN_ERR_HIP = -4          /* a HIP runtime call or kernel launch failed */
 };
 
-enum { NSN_OP_ENCODE = 0, NSN_OP_DECODE = 1, NSN_OP_CODEBOOK = 2 };
+enum { NSN_OP_ENCODE = 0, NSN_OP_DECODE = 1, NSN_OP_CODEBOOK = 2, NSN_OP_Q8_ATTENTION = 3, NSN_OP_Q8_EVICT = 4 };
 
 typedef struct nsn_shape {
   int32_t head_dim;   /* 128 */
@@ -336,6 +336,135 @@ int nsn_decode_attention_noalloc(const nsn_shape* shape, const void* codebook_de
                                  const nsn_cache* k_cache, const nsn_cache* v_cache,
                                  const int32_t* seq_lens_dev, int batch, int max_seq_len,
                                  float softmax_scale, int n_splits, float* out, void* stream);
+
+/* ---- The 8-bit cache -------------------------------------------------------------------------------
+ * A cache of one byte per channel with one fp32 scale per 64 tokens and head, for layers and models that
+ * 1 or 2 bits do not serve: keys and values are appended as they come (nsn_q8_append), single tokens and
+ * whole chunks attend to it (nsn_q8_attention), and it is cut down to a budget by the attention weights
+ * that its tokens have received (nsn_q8_evict).
+ *
+ * Record (one tensor kind, K or V), per unit (a sequence, or a physical page) and kv head:
+ *   codes   D = head_dim bytes per token; channel c of token t of the unit at byte
+ *             K:  t * D + c
+ *             V:  (t / n) * 256 + (c / m) * 16 + (t % n) * m + c % m        with n = 256 / D, m = D / 16
+ *           (V: cells of 16 bytes hold m channels of n tokens: what one lane reads of a row of cells serves
+ *           one operand of a matrix instruction without an exchange between lanes)
+ *           contiguous [batch][n_kv_heads][max_len * D], paged [n_pages][n_kv_heads][page_size * D]
+ *   scales  fp32, one per 64-token block: [batch][n_kv_heads][max_len / 64] or
+ *           [n_pages][n_kv_heads][page_size / 64]
+ *   A code c stands for scale * c:
+ *     NSN_Q8_INT8  c in -127 .. 127 (two's complement); scale = fp32(amax / 127), amax the largest magnitude
+ *                  of the block; c = x * fp32(1 / scale) rounded to nearest even
+ *     NSN_Q8_E4M3  c an e4m3 number (largest 448); scale = 2^e, the least e with amax <= 448 * 2^e;
+ *                  c = x / scale rounded to nearest even.  Between two such scales codes move exactly (but for
+ *                  those that become subnormal)
+ *     amax = 0 (or below 2^-117): scale 0, codes 0.  A NaN is stored as 0; infinities do not take part in
+ *     amax and are stored as the largest code.
+ *   block_table  paged: dev int32 [batch][max_len / page_size].  An entry outside [0, n_pages) is a page that
+ *           does not exist: its tokens are neither written nor seen nor evicted into.
+ */
+enum { NSN_Q8_INT8 = 0, NSN_Q8_E4M3 = 1 };
+enum { NSN_FP16 = 0, NSN_BF16 = 1 };
+
+typedef struct nsn_q8_shape {
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t n_q_heads;  /* a multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t code_type;  /* NSN_Q8_INT8 or NSN_Q8_E4M3 */
+  int32_t io_type;    /* NSN_FP16 or NSN_BF16: type of the new rows, the queries and the output */
+  int32_t page_size;  /* 0 = contiguous; else tokens per page, multiple of 64 */
+  int32_t n_pages;    /* paged: physical pages of the cache */
+  int32_t max_len;    /* token capacity per sequence, multiple of 64 (and of page_size) */
+} nsn_q8_shape;
+
+typedef struct nsn_q8_cache {
+  uint8_t* codes;             /* dev, 16-byte aligned */
+  float* scales;              /* dev */
+  const int32_t* block_table; /* dev, paged layout only (else NULL) */
+} nsn_q8_cache;
+
+/* Rows of head_dim consecutive 16-bit values; strides in elements, multiples of 8, data 16-byte aligned. */
+typedef struct nsn_rows {
+  const void* data; /* dev */
+  int64_t batch_stride, head_stride, token_stride;
+} nsn_rows;
+
+/* Byte offset of channel c of token t inside a unit; -1 for an invalid shape, t < 0 or c outside the head. */
+int64_t nsn_q8_k_code_offset(const nsn_q8_shape* shape, int64_t t, int c);
+int64_t nsn_q8_v_code_offset(const nsn_q8_shape* shape, int64_t t, int c);
+
+/*
+ * Device bytes an operation needs, for sequences of up to max_seq_len tokens.
+ *   NSN_OP_Q8_ATTENTION  n = n_q; n_splits as passed to nsn_q8_attention (0 = auto).  Fill the workspace with zeros
+ *                        ONCE after allocating it; every call leaves it ready for the next one, of any size.
+ *   NSN_OP_Q8_EVICT      n = keep; n_splits ignored.  Needs no preparation.
+ * It starts on a 16-byte boundary.  Calls that share a workspace must not overlap in time, and the two operations do not
+ * share one.  Returns 0 for an invalid shape or size.
+ */
+size_t nsn_q8_workspace_bytes(const nsn_q8_shape* shape, int op, int batch, int n, int max_seq_len, int n_splits);
+
+/*
+ * Writes tokens [seq_start[b], seq_start[b] + n_new[b]) of every sequence from rows 0 .. n_new[b] - 1 of k and v.
+ * Any start: where the first new token lies inside a 64-token block, the block keeps the tokens before it.  Its
+ * scale is the larger of the stored one and the one that the new tokens ask for; where it grows, the codes before
+ * are rounded again, c -> c * fp32(old / new) to nearest even.  Tokens of the block behind the last new one are left as they were.
+ *   k, v          rows by (sequence, kv head, token), at least max_new tokens each; rows >= n_new[b] are not read
+ *   seq_start, n_new  dev int32 [batch].  n_new is taken as at most max_new; a negative start or count writes nothing;
+ *                 tokens beyond max_len are not written
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int nsn_q8_append(const nsn_q8_shape* shape, const nsn_rows* k, const nsn_rows* v, int max_new,
+                  const int32_t* seq_start_dev, const int32_t* n_new_dev, int batch, const nsn_q8_cache* k_cache,
+                  const nsn_q8_cache* v_cache, void* stream);
+
+/*
+ * Attention of n_q query tokens per sequence over the cache (n_q = 1: a decode step; a chunk of a prompt whose
+ * keys and values have been appended; or a decoder's tokens over an encoder's states):
+ *   score_it = softmax_scale * q_i . k_t      out_i = sum_t softmax(score_i)_t v_t     lse_i = ln sum_t exp(score_it)
+ * over the tokens t < seq_lens[b] that query i sees: all (causal = 0), or those with
+ * t <= seq_lens[b] - q_lens[b] + i (causal = 1: the queries are the last q_lens[b] tokens of the sequence).
+ * A query that sees nothing has a zero output row and lse = -infinity.
+ *   q             rows by (sequence, query head, token); query head hq reads kv head hq / (n_q_heads / n_kv_heads)
+ *   q_lens_dev    dev int32 [batch], or NULL = n_q everywhere; queries i >= q_lens[b] are not read and their rows of
+ *                 out and lse not written
+ *   seq_lens_dev  dev int32 [batch], tokens in the cache; taken as within [0, max_seq_len]
+ *   max_seq_len   host upper bound of seq_lens (sizes the launch; <= max_len)
+ *   weights_in, weights_out  fp32 [batch][n_kv_heads][max_len], or NULL.  With weights_out,
+ *                 weights_out[b][h][t] = weights_in[b][h][t] + sum over the queries i < q_lens[b] and the query heads
+ *                 of kv head h of softmax(score_i)_t,  for t < seq_lens[b]; the rest of weights_out is not written.
+ *                 weights_in may be weights_out, or NULL (zeros).
+ *   n_splits      partitions of the token axis that are worked on at the same time and merged (0 = choose)
+ *   out           io_type [batch][n_q][n_q_heads][head_dim], 16-byte aligned
+ *   lse           fp32 [batch][n_q][n_q_heads], or NULL
+ * Scores, sums and the output are accumulated in fp32; the weights p enter the second product as fp16.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+int nsn_q8_attention(const nsn_q8_shape* shape, const nsn_rows* q, int n_q, const int32_t* q_lens_dev,
+                     const nsn_q8_cache* k_cache, const nsn_q8_cache* v_cache, const int32_t* seq_lens_dev, int batch,
+                     int max_seq_len, float softmax_scale, int causal, const float* weights_in, float* weights_out,
+                     int n_splits, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cuts every head's cache down to `keep` tokens.  A sequence of n = seq_lens[b] <= keep tokens is copied whole.  Of a longer
+ * one each kv head keeps its first `first` tokens, its last `recent` ones and, of the others, the keep - first - recent
+ * with the largest weights (equal weights: the lower index first; a NaN is the least).  The kept tokens move, in
+ * their order, to tokens 0, 1, .. of the same sequence and head in another cache.  The scale of a block there is the
+ * largest of its tokens' former scales; codes of tokens whose scale was smaller are rounded again, c -> c * fp32(former / new) to
+ * nearest even.
+ *   weights      fp32 [batch][n_kv_heads][max_len] (weights_out of nsn_q8_attention)
+ *   k_cache, v_cache  the caches read; k_out, v_out those written, of the same shape: other buffers, or (paged) the same
+ *                ones under a block table that shares no page with what is read
+ *   first, recent  >= 0, first + recent <= keep;  1 <= keep <= max_len
+ *   kept         out, int32 [batch][n_kv_heads][keep]: former indices, ascending; -1 behind the last
+ *   new_lens     out, int32 [batch] = min(seq_lens[b], keep)
+ *   weights_out  out, fp32 [batch][n_kv_heads][max_len], or NULL: the kept tokens' weights, then zeros up to max_seq_len
+ *                (not the buffer `weights`)
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+int nsn_q8_evict(const nsn_q8_shape* shape, const float* weights, const int32_t* seq_lens_dev, int batch,
+                 int max_seq_len, int keep, int first, int recent, const nsn_q8_cache* k_cache,
+                 const nsn_q8_cache* v_cache, const nsn_q8_cache* k_out, const nsn_q8_cache* v_out, int32_t* kept,
+                 int32_t* new_lens, float* weights_out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,9 @@ LIB_PATH = os.path.join(_HERE, "libnsn.so")
 
 NSN_OK = 0
 NSN_ERR_INVALID_ARG, NSN_ERR_UNSUPPORTED, NSN_ERR_WORKSPACE, NSN_ERR_HIP = -1, -2, -3, -4
-NSN_OP_ENCODE, NSN_OP_DECODE, NSN_OP_CODEBOOK = 0, 1, 2
+NSN_OP_ENCODE, NSN_OP_DECODE, NSN_OP_CODEBOOK, NSN_OP_Q8_ATTENTION, NSN_OP_Q8_EVICT = 0, 1, 2, 3, 4
+NSN_Q8_INT8, NSN_Q8_E4M3 = 0, 1
+NSN_FP16, NSN_BF16 = 0, 1
 NSN_VARIANT_DEFAULT, NSN_VARIANT_ALT = 0, 1
 HEAD_DIM, N_CODES = 128, 256
 
@@ -35,6 +37,19 @@ class nsn_cache(C.Structure):
 
 class nsn_residual(C.Structure):
     _fields_ = [("k_fp16", C.c_void_p), ("v_fp16", C.c_void_p), ("lens", C.c_void_p), ("capacity", C.c_int32)]
+
+
+class nsn_q8_shape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("head_dim", "n_q_heads", "n_kv_heads", "code_type", "io_type", "page_size", "n_pages",
+                                         "max_len")]
+
+
+class nsn_q8_cache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("block_table", C.c_void_p)]
+
+
+class nsn_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
 
 
 class NsnError(RuntimeError):
@@ -85,6 +100,19 @@ def lib() -> C.CDLL:
         L.nsn_decode_attention_noalloc.argtypes = [C.POINTER(nsn_shape), C.c_void_p, C.c_void_p,
                                                    C.POINTER(nsn_cache), C.POINTER(nsn_cache), C.c_void_p, C.c_int,
                                                    C.c_int, C.c_float, C.c_int, C.c_void_p, C.c_void_p]
+        for fn in (L.nsn_q8_k_code_offset, L.nsn_q8_v_code_offset):
+            fn.restype = C.c_int64
+            fn.argtypes = [C.c_void_p, C.c_int64, C.c_int]
+        L.nsn_q8_workspace_bytes.restype = C.c_size_t
+        L.nsn_q8_workspace_bytes.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]
+        L.nsn_q8_append.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
+                                    C.c_void_p, C.c_void_p]
+        L.nsn_q8_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                       C.c_int, C.c_float, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_size_t, C.c_void_p]
+        L.nsn_q8_evict.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                   C.c_void_p]
         _lib = L
     return _lib
 
@@ -315,3 +343,140 @@ def nsn_decode_attention_noalloc(shape: nsn_shape, codebook: torch.Tensor, q: to
                                               C.byref(vc), seq_lens.data_ptr(), batch, max_seq_len,
                                               float(softmax_scale), n_splits, out.data_ptr(), _stream()))
     return out
+
+
+# ---- the 8-bit cache ----------------------------------------------------------------------------------------------
+
+def make_q8_shape(head_dim: int, n_q_heads: int, n_kv_heads: int, max_len: int, page_size: int = 0, n_pages: int = 0,
+                  code_type: int = NSN_Q8_INT8, dtype: torch.dtype = torch.float16) -> nsn_q8_shape:
+    """code_type: NSN_Q8_INT8 or NSN_Q8_E4M3.  dtype: of new keys and values, queries and outputs (fp16 or bf16)."""
+    assert dtype in (torch.float16, torch.bfloat16), "rows are fp16 or bf16"
+    shape = nsn_q8_shape(head_dim, n_q_heads, n_kv_heads, code_type, NSN_FP16 if dtype == torch.float16 else NSN_BF16, page_size,
+                         n_pages, max_len)
+    shape.dtype = dtype
+    return shape
+
+
+class Q8Cache:
+    """Device buffers of one tensor kind (K or V) in the layout include/nsn.h documents; they stay the same for its lifetime."""
+    __slots__ = ("codes", "scales", "block_table", "c", "device")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, block_table: torch.Tensor | None = None):
+        assert codes.is_cuda and codes.dtype == torch.uint8 and codes.is_contiguous(), "codes: cuda uint8, contiguous"
+        assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.device == codes.device, "scales: fp32, contiguous"
+        assert block_table is None or (block_table.dtype == torch.int32 and block_table.is_contiguous() and
+                                       block_table.device == codes.device), "block_table: int32, contiguous"
+        self.codes, self.scales, self.block_table, self.device = codes, scales, block_table, codes.device
+        self.c = nsn_q8_cache(codes.data_ptr(), scales.data_ptr(), _ptr(block_table))
+
+
+def _q8_units(shape: nsn_q8_shape, batch: int) -> tuple[int, int]:
+    return (shape.n_pages, shape.page_size) if shape.page_size > 0 else (batch, shape.max_len)
+
+
+def alloc_q8_cache(shape: nsn_q8_shape, batch: int, device="cuda", block_table: torch.Tensor | None = None) -> Q8Cache:
+    """Zero-initialised buffers.  Paged layout: shape.n_pages physical pages and a block_table int32 [batch][max_len / page_size]."""
+    units, tokens = _q8_units(shape, batch)
+    assert shape.page_size == 0 or block_table is not None, "paged layout needs a block_table"
+    return Q8Cache(torch.zeros((units, shape.n_kv_heads, tokens, shape.head_dim), dtype=torch.uint8, device=device),
+                   torch.zeros((units, shape.n_kv_heads, tokens // 64), dtype=torch.float32, device=device), block_table)
+
+
+def nsn_q8_workspace_bytes(shape: nsn_q8_shape, op: int, batch: int, n: int, max_seq_len: int, n_splits: int = 0) -> int:
+    """op: NSN_OP_Q8_ATTENTION (n = n_q) or NSN_OP_Q8_EVICT (n = keep)."""
+    return lib().nsn_q8_workspace_bytes(C.byref(shape), op, batch, n, max_seq_len, n_splits)
+
+
+def _q8_check(shape: nsn_q8_shape, batch: int, *caches: Q8Cache) -> None:
+    device = torch._C._cuda_getDevice()
+    units, tokens = _q8_units(shape, batch)
+    for c in caches:
+        assert c.device.index == device, "the cache lies on another device than the current one"
+        assert c.codes.numel() >= units * shape.n_kv_heads * tokens * shape.head_dim, "codes: too small for the shape"
+        assert c.scales.numel() >= units * shape.n_kv_heads * (tokens // 64), "scales: too small for the shape"
+        if shape.page_size > 0:
+            assert c.block_table is not None and c.block_table.numel() >= batch * (shape.max_len // shape.page_size), \
+                "block_table: [batch][max_len / page_size] needed"
+
+
+def _q8_small(t: torch.Tensor, device, numel: int, dtype=torch.int32) -> int:
+    assert t.device == device and t.dtype == dtype and t.is_contiguous() and t.numel() >= numel, \
+        f"{numel} contiguous values of type {dtype} on {device} needed"
+    return t.data_ptr()
+
+
+def _q8_rows(t: torch.Tensor, shape: nsn_q8_shape, device, head: int, token: int) -> nsn_rows:
+    assert t.device == device and t.dtype == shape.dtype, f"rows: {shape.dtype} on {device} needed"
+    s = t.stride()
+    assert s[3] == 1, "rows: the channels of a row must be consecutive"
+    return nsn_rows(t.data_ptr(), s[0], s[head], s[token])
+
+
+def nsn_q8_append(shape: nsn_q8_shape, k: torch.Tensor, v: torch.Tensor, seq_start: torch.Tensor, n_new: torch.Tensor,
+                  k_cache: Q8Cache, v_cache: Q8Cache) -> None:
+    """k, v: cuda shape.dtype [B][Hkv][max_new][D] (any strides of whole 8-value pieces, e.g. a transposed view of
+    [B][max_new][Hkv][D]); seq_start, n_new: cuda int32 [B]."""
+    batch, hkv, max_new, d = k.shape
+    assert v.shape == k.shape and hkv == shape.n_kv_heads and d == shape.head_dim, "k, v: [batch][n_kv_heads][max_new][head_dim]"
+    _q8_check(shape, batch, k_cache, v_cache)
+    dev = k_cache.device
+    _check(lib().nsn_q8_append(C.byref(shape), C.byref(_q8_rows(k, shape, dev, 1, 2)), C.byref(_q8_rows(v, shape, dev, 1, 2)), max_new,
+                               _q8_small(seq_start, dev, batch), _q8_small(n_new, dev, batch), batch, C.byref(k_cache.c),
+                               C.byref(v_cache.c), _stream()))
+
+
+def nsn_q8_attention(shape: nsn_q8_shape, q: torch.Tensor, k_cache: Q8Cache, v_cache: Q8Cache, seq_lens: torch.Tensor,
+                     max_seq_len: int, softmax_scale: float, causal: bool = False, q_lens: torch.Tensor | None = None,
+                     weights_in: torch.Tensor | None = None, weights_out: torch.Tensor | None = None, n_splits: int = 0,
+                     out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """q: cuda shape.dtype [B][n_q][Hq][D] (any strides of whole 8-value pieces); returns shape.dtype [B][n_q][Hq][D] (rows of
+    queries >= q_lens[b] are not written: zeros where `out` is made here).  lse: fp32 [B][n_q][Hq].
+    weights_in, weights_out: fp32 [B][Hkv][max_len].  workspace: zero-filled once (made here if there is none)."""
+    batch, n_q, hq, d = q.shape
+    assert hq == shape.n_q_heads and d == shape.head_dim, "q: [batch][n_q][n_q_heads][head_dim]"
+    _q8_check(shape, batch, k_cache, v_cache)
+    dev = k_cache.device
+    if out is None:
+        out = (torch.empty if q_lens is None else torch.zeros)((batch, n_q, hq, d), dtype=shape.dtype, device=dev)
+    if workspace is None:
+        need = nsn_q8_workspace_bytes(shape, NSN_OP_Q8_ATTENTION, batch, n_q, max_seq_len, n_splits)
+        workspace = torch.zeros(max(need, 1), dtype=torch.uint8, device=dev)
+    n_w = batch * shape.n_kv_heads * shape.max_len
+    _check(lib().nsn_q8_attention(C.byref(shape), C.byref(_q8_rows(q, shape, dev, 2, 1)), n_q,
+                                  None if q_lens is None else _q8_small(q_lens, dev, batch), C.byref(k_cache.c), C.byref(v_cache.c),
+                                  _q8_small(seq_lens, dev, batch), batch, max_seq_len, float(softmax_scale), int(causal),
+                                  None if weights_in is None else _q8_small(weights_in, dev, n_w, torch.float32),
+                                  None if weights_out is None else _q8_small(weights_out, dev, n_w, torch.float32), n_splits,
+                                  _q8_small(out, dev, q.numel(), shape.dtype),
+                                  None if lse is None else _q8_small(lse, dev, batch * n_q * hq, torch.float32),
+                                  _q8_small(workspace, dev, 0, torch.uint8), workspace.numel(), _stream()))
+    return out
+
+
+def nsn_q8_evict(shape: nsn_q8_shape, weights: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int, keep: int, k_cache: Q8Cache,
+                 v_cache: Q8Cache, k_out: Q8Cache, v_out: Q8Cache, first: int = 0, recent: int = 0,
+                 kept: torch.Tensor | None = None, new_lens: torch.Tensor | None = None, weights_out: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None):
+    """weights: cuda fp32 [B][Hkv][max_len].  Returns (kept int32 [B][Hkv][keep], new_lens int32 [B], weights_out fp32
+    [B][Hkv][max_len]); k_out, v_out are other caches of the same shape (paged: or the same pages under another block table)."""
+    batch, hkv = weights.shape[:2]
+    assert hkv == shape.n_kv_heads, "weights: [batch][n_kv_heads][max_len]"
+    _q8_check(shape, batch, k_cache, v_cache, k_out, v_out)
+    dev = k_cache.device
+    if kept is None:
+        kept = torch.empty((batch, hkv, max(keep, 0)), dtype=torch.int32, device=dev)
+    if new_lens is None:
+        new_lens = torch.empty(batch, dtype=torch.int32, device=dev)
+    if weights_out is None:
+        weights_out = torch.zeros_like(weights)
+    if workspace is None:
+        need = nsn_q8_workspace_bytes(shape, NSN_OP_Q8_EVICT, batch, keep, max_seq_len)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    n_w = batch * hkv * shape.max_len
+    _check(lib().nsn_q8_evict(C.byref(shape), _q8_small(weights, dev, n_w, torch.float32), _q8_small(seq_lens, dev, batch), batch,
+                              max_seq_len, keep, first, recent, C.byref(k_cache.c), C.byref(v_cache.c), C.byref(k_out.c),
+                              C.byref(v_out.c), _q8_small(kept, dev, batch * hkv * keep), _q8_small(new_lens, dev, batch),
+                              _q8_small(weights_out, dev, n_w, torch.float32), _q8_small(workspace, dev, 0, torch.uint8),
+                              workspace.numel(), _stream()))
+    return kept, new_lens, weights_out

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libnsn.so")
 SOURCES = ["nsn_api.hip", "nsn_encode.hip", "nsn_decode.hip", "nsn_decode_tile.hip", "nsn_decode_tile_many.hip",
-           "nsn_decode_rows.hip", "nsn_codebook.hip", "nsn_rope.hip"]
+           "nsn_decode_rows.hip", "nsn_codebook.hip", "nsn_rope.hip", "nsn_q8_api.hip", "nsn_q8_cache.hip", "nsn_q8_attention.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,146 @@
+"""The 8-bit cache's entry points without a GPU: exported symbols, layout, workspace sizes, and the refusal of every bad argument
+before anything is launched."""
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+
+from paper_2505_18231_amd import api
+from tests import q8_reference as R
+
+FAKE = 0x10000   # an aligned address that no call may reach
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(api.LIB_PATH):
+        from paper_2505_18231_amd.build import build_library
+        build_library(verbose=False)
+    return api.lib()
+
+
+def shape(**kw):
+    s = api.make_q8_shape(128, 32, 8, 1024)
+    for k, v in kw.items():
+        setattr(s, k, v)
+    return s
+
+
+def cache(**kw):
+    c = api.nsn_q8_cache(FAKE, FAKE, None)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def rows(data=FAKE, b=0, h=128, t=1024):
+    return api.nsn_rows(data, b, h, t)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_offsets_are_the_header_s_and_a_bijection(L, D):
+    s = api.make_q8_shape(D, 8, 2, 256)
+    for kind, fn in (("k", L.nsn_q8_k_code_offset), ("v", L.nsn_q8_v_code_offset)):
+        got = np.array([[fn(C.byref(s), t, c) for c in range(D)] for t in range(128)])
+        assert np.array_equal(got, R.offsets(kind, D, 128))
+        assert sorted(got.ravel().tolist()) == list(range(128 * D))
+        assert fn(C.byref(s), -1, 0) == -1 and fn(C.byref(s), 0, D) == -1 and fn(C.byref(s), 0, -1) == -1
+    assert L.nsn_q8_v_code_offset(C.byref(s), (1 << 40) + 1, 0) == (1 << 40) * D + (D // 16)
+
+
+BAD_SHAPES = [(dict(head_dim=96), -2), (dict(code_type=2), -2), (dict(io_type=2), -2), (dict(io_type=-1), -2), (dict(n_q_heads=12), -1),
+              (dict(n_kv_heads=0), -1), (dict(n_q_heads=0), -1), (dict(n_q_heads=65536, n_kv_heads=1), -1), (dict(max_len=100), -1),
+              (dict(max_len=0), -1), (dict(page_size=48), -1), (dict(page_size=-64), -1), (dict(page_size=192, n_pages=5), -1),
+              (dict(page_size=64, n_pages=0), -1)]
+
+
+def append(L, s, k=None, v=None, max_new=4, start=FAKE, n=FAKE, batch=1, kc=None, vc=None):
+    return L.nsn_q8_append(C.byref(s), C.byref(k or rows()), C.byref(v or rows()), max_new, start, n, batch,
+                           C.byref(kc or cache()), C.byref(vc or cache()), None)
+
+
+def attend(L, s, q=None, n_q=1, q_lens=None, kc=None, vc=None, lens=FAKE, batch=1, max_seq=1024, scale=1.0, w_in=None, w_out=None,
+           splits=0, out=FAKE, lse=None, ws=FAKE, ws_bytes=1 << 40):
+    return L.nsn_q8_attention(C.byref(s), C.byref(q or rows()), n_q, q_lens, C.byref(kc or cache()), C.byref(vc or cache()), lens, batch,
+                              max_seq, scale, 0, w_in, w_out, splits, out, lse, ws, ws_bytes, None)
+
+
+def evict(L, s, w=FAKE, lens=FAKE, batch=1, max_seq=1024, keep=64, first=0, recent=0, kc=None, vc=None, ko=None, vo=None, kept=FAKE,
+          new=FAKE, w_out=None, ws=FAKE, ws_bytes=1 << 40):
+    far = 1 << 44
+    return L.nsn_q8_evict(C.byref(s), w, lens, batch, max_seq, keep, first, recent, C.byref(kc or cache(codes=far, scales=far)),
+                          C.byref(vc or cache(codes=2 * far, scales=2 * far)), C.byref(ko or cache(codes=3 * far, scales=3 * far)),
+                          C.byref(vo or cache(codes=4 * far, scales=4 * far)), kept, new, w_out, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,rc", BAD_SHAPES)
+def test_bad_shapes_are_refused_everywhere(L, kw, rc):
+    s = shape(**kw)
+    assert append(L, s) == rc and attend(L, s) == rc and evict(L, s) == rc and L.nsn_last_error()
+    for op in (api.NSN_OP_Q8_ATTENTION, api.NSN_OP_Q8_EVICT):
+        assert api.nsn_q8_workspace_bytes(s, op, 1, 1, 64) == 0
+    assert L.nsn_q8_k_code_offset(C.byref(s), 0, 0) == -1 and L.nsn_q8_v_code_offset(C.byref(s), 0, 0) == -1
+    assert L.nsn_q8_append(None, C.byref(rows()), C.byref(rows()), 1, FAKE, FAKE, 1, C.byref(cache()), C.byref(cache()), None) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(codes=None), dict(scales=None), dict(codes=FAKE + 8), dict(scales=FAKE + 2)])
+def test_bad_caches_are_refused(L, kw):
+    s = shape()
+    for name in ("kc", "vc"):
+        for call in (append, attend, evict):
+            assert call(L, s, **{name: cache(**kw)}) == -1
+    for name in ("ko", "vo"):
+        assert evict(L, s, **{name: cache(**kw)}) == -1
+    paged = shape(page_size=64, n_pages=3)
+    for call in (append, attend, evict):
+        assert call(L, paged) == -1 and b"block_table" in L.nsn_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(data=None), dict(data=FAKE + 2), dict(b=4), dict(h=129), dict(t=1020)])
+def test_rows_that_are_not_aligned_are_refused(L, bad):
+    s = shape()
+    assert append(L, s, k=rows(**bad)) == -1 and append(L, s, v=rows(**bad)) == -1 and attend(L, s, q=rows(**bad)) == -1
+    assert b"rows" in L.nsn_last_error()
+
+
+def test_other_arguments_are_refused(L):
+    s = shape()
+    for kw in (dict(start=None), dict(n=None), dict(batch=-1), dict(batch=65536), dict(max_new=-1)):
+        assert append(L, s, **kw) == -1, kw
+    assert append(L, s, batch=0) == 0 and append(L, s, max_new=0) == 0
+    for kw in (dict(lens=None), dict(out=None), dict(out=FAKE + 2), dict(batch=-1), dict(batch=65536), dict(n_q=-1), dict(splits=-1),
+               dict(max_seq=-1), dict(max_seq=1025), dict(scale=float("nan")), dict(scale=float("inf")), dict(w_in=FAKE),
+               dict(n_q=0, w_out=FAKE)):
+        assert attend(L, s, **kw) == -1, kw
+    assert attend(L, s, batch=0) == 0 and attend(L, s, n_q=0) == 0
+    assert attend(L, s, n_q=1 << 23) == api.NSN_ERR_UNSUPPORTED
+    need = api.nsn_q8_workspace_bytes(s, api.NSN_OP_Q8_ATTENTION, 1, 1, 1024)
+    assert need > 0
+    for kw in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=FAKE + 8)):
+        assert attend(L, s, **kw) == api.NSN_ERR_WORKSPACE, kw
+    for kw in (dict(w=None), dict(lens=None), dict(kept=None), dict(new=None), dict(batch=-1), dict(batch=65536), dict(max_seq=1025),
+               dict(max_seq=-1), dict(keep=0), dict(keep=1025), dict(first=-1), dict(recent=-1), dict(first=40, recent=25), dict(w_out=FAKE)):
+        assert evict(L, s, **kw) == -1, kw
+    assert evict(L, s, batch=0) == 0
+    assert api.nsn_q8_workspace_bytes(s, api.NSN_OP_ENCODE, 1, 1, 64) == 0
+
+
+def test_an_eviction_into_the_cache_that_it_reads_is_refused(L):
+    s, far = shape(), 1 << 44
+    one = lambda i, d=0: cache(codes=i * far + d, scales=i * far + d)  # noqa: E731
+    for a in ("kc", "vc"):
+        for b in ("ko", "vo"):
+            assert evict(L, s, **{a: one(9), b: one(9)}) == -1, (a, b)
+            assert evict(L, s, **{a: one(9), b: one(9, 4096)}) == -1, (a, b)       # overlapping, not the same
+            assert evict(L, s, **{a: one(9, 4096), b: one(9)}) == -1, (a, b)
+    assert evict(L, s, ko=one(9), vo=one(9)) == -1
+    paged = shape(page_size=64, n_pages=8)
+    t = lambda i, table: cache(codes=i * far, scales=i * far, block_table=table)  # noqa: E731
+    assert evict(L, paged, kc=t(1, FAKE), vc=t(2, FAKE), ko=t(1, FAKE), vo=t(2, 2 * FAKE)) == -1
+    assert evict(L, paged, kc=t(1, FAKE), vc=t(2, FAKE), ko=t(1, 2 * FAKE), vo=t(2, FAKE)) == -1
+
+
+def test_shape_of_the_python_form():
+    with pytest.raises(AssertionError):
+        api.make_q8_shape(128, 8, 8, 1024, dtype=__import__("torch").float32)

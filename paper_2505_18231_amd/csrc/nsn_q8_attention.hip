@@ -58,9 +58,40 @@ __device__ __forceinline__ int visible(const Args& a, const Problem& p, int i) {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Rows of queries as fp16 operands: w holds this lane's pieces of one row, whose other pieces lie in the lanes LANES apart.  Returns the
+// factor (not negative: a negative softmax scale turns the row's signs) that takes q . k to a power of two.
+template <bool BF, int N, int LANES>
+__device__ __forceinline__ float query_operands(float scale, uint4v (&w)[N], half8v (&q)[N]) {
+  if (scale < 0.f) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) w[s] ^= 0x80008000u;
+    scale = -scale;
+  }
+  if constexpr (!BF) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) q[s] = __builtin_bit_cast(half8v, w[s]);
+    return scale;
+  } else {
+    float amax = 0.f;
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(__uint_as_float(e & 1 ? w[s][e / 2] & 0xffff0000u : w[s][e / 2] << 16)));
+#pragma unroll
+    for (int d = LANES; d < 64; d *= 2) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
+    const int e2 = amax > 0.f ? 15 - __builtin_amdgcn_frexp_expf(amax) : 0;  // (an infinity or NaN: frexp gives 0)
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        q[s][e] = (_Float16)ldexpf(__uint_as_float(e & 1 ? w[s][e / 2] & 0xffff0000u : w[s][e / 2] << 16), e2);
+    return ldexpf(scale, -e2);
+  }
+}
+
 // The 16 rows r0 .. r0 + 15 as the second operand of the 16x16x32 products: lane 16 kg + n holds row n, and of every 64
 // channels the 16 from 16 kg on, which is how a lane reads a row of key codes in 16-byte pieces (the order of the channels in
-// a product is free as long as both operands share it).  Returns the factor that takes q . k to a power of two.
+// a product is free as long as both operands share it).
 template <int D, bool BF>
 __device__ __forceinline__ float load_queries(const Args& a, int b, int h, int r, int nq, half8v (&q)[D / 32]) {
   const int kg = (threadIdx.x & 63) >> 4;
@@ -70,26 +101,19 @@ __device__ __forceinline__ float load_queries(const Args& a, int b, int h, int r
   uint4v w[D / 32];
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) w[s] = there ? *reinterpret_cast<const uint4v*>(p + (s >> 1) * 64 + (s & 1) * 8) : uint4v{0, 0, 0, 0};
-  if constexpr (!BF) {
+  return query_operands<BF, D / 32, 16>(a.scale_log2, w, q);
+}
+
+// The same for the 32x32x16 products: row r in lanes n and 32 + n, channels 16 s + 8 (lane / 32) + 0 .. 7 in operand s.
+template <int D, bool BF>
+__device__ __forceinline__ float load_query_rows(const Args& a, int b, int h, int r, int nq, half8v (&q)[D / 16]) {
+  const bool there = r < nq * a.g.ratio;
+  const int i = there ? r / a.g.ratio : 0, hq = there ? h * a.g.ratio + r % a.g.ratio : 0;
+  const uint16_t* p = a.q.data + b * a.q.sb + hq * a.q.sh + i * a.q.st + 8 * ((threadIdx.x & 63) >> 5);
+  uint4v w[D / 16];
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) q[s] = __builtin_bit_cast(half8v, w[s]);
-    return a.scale_log2;
-  } else {
-    float amax = 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(__uint_as_float(e & 1 ? w[s][e / 2] & 0xffff0000u : w[s][e / 2] << 16)));
-    amax = fmaxf(amax, __shfl_xor(amax, 16, 64));
-    amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
-    const int e2 = amax > 0.f ? 15 - __builtin_amdgcn_frexp_expf(amax) : 0;  // (an infinity or NaN: frexp gives 0)
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        q[s][e] = (_Float16)ldexpf(__uint_as_float(e & 1 ? w[s][e / 2] & 0xffff0000u : w[s][e / 2] << 16), e2);
-    return ldexpf(a.scale_log2, -e2);
-  }
+  for (int s = 0; s < D / 16; ++s) w[s] = there ? *reinterpret_cast<const uint4v*>(p + 16 * s) : uint4v{0, 0, 0, 0};
+  return query_operands<BF, D / 16, 32>(a.scale_log2, w, q);
 }
 
 // key codes of a block as the first operand: tile j = tokens 16 j .. 16 j + 15, lane 16 kg + n: token 16 j + n
@@ -294,6 +318,236 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(Args a) {
   }
 }
 
+// ---- many rows: tiles in LDS ------------------------------------------------------------------------------
+// One workgroup of four waves per 128 rows (and split), a wave holding 32 of them.  Each 64-token tile of keys and values is
+// converted once per workgroup and staged in LDS as fp16: keys token by token, values transposed, in the order in which the score
+// product leaves the weights in a lane, so that both products read their first operand as 16-byte rows and the weights never
+// leave their lane.  The next tile's codes are on their way to registers while a tile is worked on; two tiles in LDS, one barrier a tile.
+//
+// The output accumulates in the matrix registers from tile to tile without a pass over it:
+//   - the running maximum is moved (and the sums rescaled) only when a row's scores pass it by 2^kLazy;
+//   - a tile's value scale sv enters the exponent, p' = 2^(s - m + kLift + log2(sv / sref)), against a power of two sref that
+//     follows sv when it is off by more than 2^kSpan.  p' stays below 2^(kLift + kLazy + kSpan + 1) <= 2^15, and weights down to 2^-20 of
+//     the row's largest one are normal fp16 numbers.
+constexpr int kLazy = 4, kSpan = 4, kLift = 6;
+
+template <int D>
+struct ChunkTile {
+  static constexpr int kKeyRow = D + 8, kValRow = kBlock + 8;  // halves per row: 16 bytes more, so that rows start on other banks
+  _Float16 k[kBlock][kKeyRow];
+  _Float16 v[D][kValRow];  // row 16 i + n: channel (D / 16) n + i; place 16 st + 8 hh + j: token 16 st + 8 (j / 4) + 4 hh + j % 4
+};
+
+template <int D, int CODE, bool BF>
+__global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
+  constexpr int kCh = D / 16, kTok = 256 / D, kCellsOf4 = 4 / kTok, kKeyCells = D / 64;
+  __shared__ ChunkTile<D> sm[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hh = lane >> 5, n = lane & 31;
+  // (sequence, head, split) is the fastest index: workgroups that read the same keys fall on the same compute die where their
+  // number is a multiple of eight; the last tiles, which see most under a causal mask, come first
+  const int units = a.g.hkv * a.n_splits, tiles = (a.rows + 32 * kWaves - 1) / (32 * kWaves);
+  const int unit = blockIdx.x % units, tile = tiles - 1 - blockIdx.x / units, b = blockIdx.y;
+  const int h = unit % a.g.hkv, split = unit / a.g.hkv;
+  const Problem pr = problem_of(a, b);
+  const int n_rows = pr.nq * a.g.ratio, r0 = tile * 32 * kWaves;
+  if (r0 >= n_rows) return;
+  const int rw = r0 + wave * 32, r = rw + n;
+  const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : pr.len;
+  // what the wave's and the workgroup's rows see at least and at most
+  const int last = min(rw + 31, n_rows - 1);
+  const int vis_min = rw < n_rows ? visible(a, pr, rw / a.g.ratio) : 0, vis_max = rw < n_rows ? visible(a, pr, last / a.g.ratio) : 0;
+  const int vis_all = visible(a, pr, min(r0 + 32 * kWaves - 1, n_rows - 1) / a.g.ratio);
+  const int blk0 = split * a.per, blk1 = min(blk0 + a.per, (vis_all + kBlock - 1) / kBlock);
+
+  half8v q[D / 16];
+  const float factor = load_query_rows<D, BF>(a, b, h, r, pr.nq, q);
+  float m = -INFINITY, l = 0.f, sref = 0.f;
+  float16v o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+
+  // this thread's part of a tile: 16-byte pieces of key codes, and four tokens of a column of value cells
+  const int vn = tid & 15, vhalf = (tid >> 4) & 1, vh = (tid >> 5) & 1, vst = tid >> 6, vt = 16 * vst + 8 * vhalf + 4 * vh;
+  uint4v kw[kKeyCells], vw[kCellsOf4];
+  float next_sk = 0.f, next_sv = 0.f;
+  bool next_there = false;
+  auto fetch = [&](int blk) {
+    const int64_t pk = block_place(a.g, a.kc.block_table, b, h, blk), pv = block_place(a.g, a.vc.block_table, b, h, blk);
+    next_there = pk >= 0 && pv >= 0;
+    if (!next_there) return;
+    const uint8_t* kp = a.kc.codes + pk * (int64_t)(kBlock * D);
+    const uint8_t* vp = a.vc.codes + pv * (int64_t)(kBlock * D);
+#pragma unroll
+    for (int i = 0; i < kKeyCells; ++i) kw[i] = *reinterpret_cast<const uint4v*>(kp + (tid + i * kWaves * 64) * 16);
+#pragma unroll
+    for (int c = 0; c < kCellsOf4; ++c) vw[c] = *reinterpret_cast<const uint4v*>(vp + (vt / kTok + c) * 256 + vn * 16);
+    next_sk = a.kc.scales[pk], next_sv = a.vc.scales[pv];
+    if (CODE == NSN_Q8_E4M3 && (blk + 1) * kBlock > pr.len) {  // places behind the last token may hold NaN: 0 * NaN is one
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (blk * kBlock + vt + t >= pr.len) {
+#pragma unroll
+          for (int e = 0; e < 4 / kTok; ++e) vw[t / kTok][t % kTok * (4 / kTok) + e] = 0;
+        }
+    }
+  };
+  auto stage = [&](ChunkTile<D>& to) {
+#pragma unroll
+    for (int i = 0; i < kKeyCells; ++i) {
+      const int cell = tid + i * kWaves * 64;
+      _Float16* p = &to.k[cell / kCh][cell % kCh * 16];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        half2v u0, u1, u2, u3;
+        to_half4<CODE>(kw[i][2 * x], u0, u1);
+        to_half4<CODE>(kw[i][2 * x + 1], u2, u3);
+        *reinterpret_cast<half8v*>(p + 8 * x) = half8v{u0[0], u0[1], u1[0], u1[1], u2[0], u2[1], u3[0], u3[1]};
+      }
+    }
+#pragma unroll
+    for (int c2 = 0; c2 < kCh / 2; ++c2) {
+      half2v x[2], y[2];
+#pragma unroll
+      for (int pair = 0; pair < 2; ++pair) {
+        const int t = 2 * pair;
+        const unsigned u = vw[t / kTok][t % kTok * (4 / kTok) + c2 / 2], w = vw[(t + 1) / kTok][(t + 1) % kTok * (4 / kTok) + c2 / 2];
+        to_half4<CODE>(__builtin_amdgcn_perm(w, u, c2 & 1 ? 0x07030602u : 0x05010400u), x[pair], y[pair]);
+      }
+      const int at = 16 * vst + 8 * vh + 4 * vhalf;
+      *reinterpret_cast<half4v*>(&to.v[16 * (2 * c2) + vn][at]) = half4v{x[0][0], x[0][1], x[1][0], x[1][1]};
+      *reinterpret_cast<half4v*>(&to.v[16 * (2 * c2 + 1) + vn][at]) = half4v{y[0][0], y[0][1], y[1][0], y[1][1]};
+    }
+  };
+
+  if (blk0 < blk1) {
+    fetch(blk0);
+    if (next_there) stage(sm[0]);
+  }
+  for (int blk = blk0, buf = 0; blk < blk1; ++blk, buf ^= 1) {
+    const bool there = next_there;
+    const float sk = next_sk, sv = next_sv;
+    const int t0 = blk * kBlock;
+    __syncthreads();  // the tile is complete, and everybody has left the one before it
+    if (blk + 1 < blk1) fetch(blk + 1);
+    if (there && t0 < vis_max) {
+      const ChunkTile<D>& tl = sm[buf];
+      float16v s[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8v*>(&tl.k[32 * j + n][16 * ks + 8 * hh]), q[ks], s[j], 0, 0, 0);
+      }
+      const float f = factor * sk;
+      const bool masked = t0 + kBlock > vis_min;
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) s[j][e] = -1e30f;  // (finite: f may be 0)
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[j][e]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * f;
+      if (__any(top > m + kLazy)) {  // (each row by its own scores: its result does not hang on its neighbours)
+        const float m_new = top > m + kLazy ? top : m;
+        const float alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+      }
+      float ratio = 1.f, lift = kLift;  // sref / sv, kLift + log2(sv / sref)
+      if (sv > 0.f) {
+        // (a jump of more than 2^60 downwards would take the sums out of range: weights that small count as they underflow)
+        if (!(sv <= sref * (1 << kSpan) && sv * (1 << kSpan) >= sref) && !(sv < sref * 0x1p-60f)) {
+          const float now = ldexpf(0.5f, __builtin_amdgcn_frexp_expf(sv));
+          const float turn = sref > 0.f ? sref / now : 0.f;
+          sref = now;
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[i][e] *= turn;
+        }
+        ratio = sref / sv;
+        lift = kLift + __log2f(sv / sref);
+      }
+      const float base = m - lift;
+      float sum[2] = {0.f, 0.f};
+      half8v p[4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          float x = fast_exp2(fmaf(s[j][e], f, -base)), y = fast_exp2(fmaf(s[j][e + 1], f, -base));
+          if (masked) {
+            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) x = 0.f;
+            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 + 1 >= vis) y = 0.f;
+          }
+          sum[0] += x, sum[1] += y;
+          const half2v u = __builtin_convertvector((float2v{x, y}), half2v);
+          p[2 * j + e / 8][e % 8] = u[0], p[2 * j + e / 8][e % 8 + 1] = u[1];
+        }
+      l = fmaf(sum[0] + sum[1], ratio, l);
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+          o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8v*>(&tl.v[32 * i + n][16 * st + 8 * hh]), p[st], o[i], 0, 0, 0);
+    }
+    if (blk + 1 < blk1 && next_there) stage(sm[buf ^ 1]);
+  }
+  if (r >= n_rows) return;
+  l += __shfl_xor(l, 32, 64);
+  // o[i][e]: row 32 i + 8 (e / 4) + 4 hh + e % 4 of the transposed values; the channels of cell c are its rows 16 x + c
+  const int64_t line = ((int64_t)b * a.g.hkv + h) * a.rows + r;
+  const float M = m - kLift;
+  const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;
+  const float inv = a.n_splits > 1 ? sref : l > 0.f ? sref / l : (l == 0.f ? 0.f : l);
+#pragma unroll
+  for (int c4 = 0; c4 < 2; ++c4)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int cell = 8 * c4 + 4 * hh + e;
+      float x[kCh];
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) x[i] = o[i / 2][8 * (i & 1) + 4 * c4 + e] * inv;
+      if (a.n_splits > 1) {
+        float* P = a.partial + (line * a.n_splits + split) * (D + 2) + kCh * cell;
+#pragma unroll
+        for (int i = 0; i < kCh; i += 2) *reinterpret_cast<float2v*>(P + i) = float2v{x[i], x[i + 1]};
+      } else {
+        alignas(16) uint16_t u[kCh];
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) u[i] = from_float<BF>(x[i]);
+        if constexpr (kCh == 8)
+          *reinterpret_cast<uint4v*>(a.out + place * D + kCh * cell) = *reinterpret_cast<const uint4v*>(u);
+        else
+          *reinterpret_cast<uint2v*>(a.out + place * D + kCh * cell) = *reinterpret_cast<const uint2v*>(u);
+      }
+    }
+  if (hh == 0) {
+    if (a.n_splits > 1) {
+      float* P = a.partial + (line * a.n_splits + split) * (D + 2);
+      P[D] = l == 0.f ? -INFINITY : M, P[D + 1] = l;
+    } else {
+      const float z = l == 0.f ? -INFINITY : M + __log2f(l);
+      if (a.lse) a.lse[place] = z * kLn2;
+      if (a.lse2) a.lse2[line] = z;
+    }
+  }
+}
+
 // the splits of a row are joined: one workgroup of D threads per row
 template <int D, bool BF>
 __global__ __launch_bounds__(D) void merge_kernel(Args a) {
@@ -373,11 +627,18 @@ __global__ __launch_bounds__(kWaves * 64) void weights_kernel(Args a) {
 }
 
 // ---- host side --------------------------------------------------------------------------------------------
+// from this many rows of a (sequence, kv head) on, tiles in LDS
+static bool use_chunk(int64_t rows) { return rows > 32; }
+
 static int split_count(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int requested) {
   const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
   if (requested > 0) return std::min(requested, blocks);
-  const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads), groups = (rows + 15) / 16 * s.n_kv_heads * batch;
-  const int64_t most = (blocks + kWaves - 1) / kWaves;
+  const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads);
+  if (use_chunk(rows)) {
+    const int64_t groups = (rows + 32 * kWaves - 1) / (32 * kWaves) * s.n_kv_heads * batch;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, 512 / groups));
+  }
+  const int64_t groups = (rows + 15) / 16 * s.n_kv_heads * batch, most = (blocks + kWaves - 1) / kWaves;
   return (int)std::max<int64_t>(1, std::min<int64_t>(most, 1024 / groups));
 }
 
@@ -409,12 +670,16 @@ int attention_launch(const AttentionCall& c) {
   return with_types(s, [&](auto d, auto code, auto bf) -> int {
     constexpr int D = decltype(d)::value, CODE = decltype(code)::value;
     constexpr bool BF = decltype(bf)::value;
-    const int tiles = (a.rows + 15) / 16;
+    const bool chunk = use_chunk(a.rows);
+    const int tiles = chunk ? (a.rows + 32 * kWaves - 1) / (32 * kWaves) : (a.rows + 15) / 16;
     if ((int64_t)tiles * a.g.hkv * a.n_splits > 0x7fffffff || (int64_t)a.rows * a.g.hkv > 0x7fffffff) {
       set_error("q8_attention: n_q * n_q_heads * n_splits is too large for one launch");
       return NSN_ERR_UNSUPPORTED;
     }
-    rows_kernel<D, CODE, BF><<<dim3(tiles * a.g.hkv * a.n_splits, c.batch), kWaves * 64, 0, c.stream>>>(a);
+    if (chunk)
+      chunk_kernel<D, CODE, BF><<<dim3(tiles * a.g.hkv * a.n_splits, c.batch), kWaves * 64, 0, c.stream>>>(a);
+    else
+      rows_kernel<D, CODE, BF><<<dim3(tiles * a.g.hkv * a.n_splits, c.batch), kWaves * 64, 0, c.stream>>>(a);
     if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
     if (a.n_splits > 1) {
       merge_kernel<D, BF><<<dim3(a.rows * a.g.hkv, c.batch), D, 0, c.stream>>>(a);

@@ -56,6 +56,9 @@ __device__ __forceinline__ int visible(const Args& a, const Problem& p, int i) {
   return a.causal ? min(max(p.vis0 + i, 0), p.len) : p.len;
 }
 
+// the wave's number in a scalar register, so that what follows from it is worked out once per wave
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Rows of queries as fp16 operands: w holds this lane's pieces of one row, whose other pieces lie in the lanes LANES apart.  Returns the
@@ -191,7 +194,7 @@ constexpr int kWaves = 4;
 template <int D, int CODE, bool BF>
 __global__ __launch_bounds__(kWaves * 64) void rows_kernel(Args a) {
   constexpr int kCh = D / 16;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = lane >> 4, n = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), kg = lane >> 4, n = lane & 15;
   const int split = blockIdx.x % a.n_splits, unit = blockIdx.x / a.n_splits;
   const int h = unit % a.g.hkv, tile = unit / a.g.hkv, b = blockIdx.y;
   const Problem pr = problem_of(a, b);
@@ -342,7 +345,7 @@ template <int D, int CODE, bool BF>
 __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
   constexpr int kCh = D / 16, kTok = 256 / D, kCellsOf4 = 4 / kTok, kKeyCells = D / 64;
   __shared__ ChunkTile<D> sm[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hh = lane >> 5, n = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), hh = lane >> 5, n = lane & 31;
   // (sequence, head, split) is the fastest index: workgroups that read the same keys fall on the same compute die where their
   // number is a multiple of eight; the last tiles, which see most under a causal mask, come first
   const int units = a.g.hkv * a.n_splits, tiles = (a.rows + 32 * kWaves - 1) / (32 * kWaves);
@@ -488,14 +491,20 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
+        for (int e = 0; e < 16; ++e) s[j][e] = fast_exp2(fmaf(s[j][e], f, -base));
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) s[j][e] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          float x = fast_exp2(fmaf(s[j][e], f, -base)), y = fast_exp2(fmaf(s[j][e + 1], f, -base));
-          if (masked) {
-            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) x = 0.f;
-            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 + 1 >= vis) y = 0.f;
-          }
-          sum[0] += x, sum[1] += y;
-          const half2v u = __builtin_convertvector((float2v{x, y}), half2v);
+          sum[0] += s[j][e], sum[1] += s[j][e + 1];
+          const half2v u = __builtin_convertvector((float2v{s[j][e], s[j][e + 1]}), half2v);
           p[2 * j + e / 8][e % 8] = u[0], p[2 * j + e / 8][e % 8 + 1] = u[1];
         }
       l = fmaf(sum[0] + sum[1], ratio, l);
@@ -579,7 +588,7 @@ __global__ __launch_bounds__(D) void merge_kernel(Args a) {
 // time, add 2^(s - lse) up per token, and are joined in a fixed order.
 template <int D, int CODE, bool BF>
 __global__ __launch_bounds__(kWaves * 64) void weights_kernel(Args a) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = lane >> 4, n = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), kg = lane >> 4, n = lane & 15;
   const int blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const Problem pr = problem_of(a, b);
   const int t0 = blk * kBlock, n_rows = pr.nq * a.g.ratio;

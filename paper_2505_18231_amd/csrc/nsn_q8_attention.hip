@@ -36,9 +36,16 @@ struct Args {
   float* lse;
   float* lse2;     // [batch][hkv][rows], in powers of two (workspace)
   float* partial;  // [batch][hkv][rows][split][D + 2] (workspace)
+  int* counters;   // [batch][row tile][hkv], one per 64 bytes: splits that have arrived (workspace)
+  int row_tiles;
+  float* scores;   // [batch][hkv][rows][score_stride] in powers of two, -infinity where nothing is seen (workspace), or NULL
+  int64_t score_stride;
   const float* weights_in;
   float* weights_out;
 };
+
+constexpr int kWaves = 4;
+constexpr int kCounterInts = 16, kMaxCounters = 2048;  // (the workspace starts with them, in every call's layout)
 
 // what a (sequence, kv head) is asked
 struct Problem {
@@ -188,11 +195,52 @@ struct ValueCodes {
 };
 
 // ---- few rows: the token axis is split -------------------------------------------------------------------
-// One workgroup of four waves per (16 rows, split); the waves take the split's blocks in turn and are joined through LDS.
-constexpr int kWaves = 4;
+// One workgroup of four waves per (16 rows, split); the waves take the split's blocks in turn, each with the next block's codes on
+// their way to registers while it works on one, and are joined through LDS.  The splits of a tile of rows are joined by the last
+// workgroup that arrives.  Bound by memory: every code is read once, and the conversions and products of a block fill a
+// third of the time that its bytes take.
+constexpr int kRowsLift = 12;  // weights are 2^kRowsLift at most: those down to 2^-26 of the largest are normal fp16 numbers
+
+template <int D>
+struct Fetched {
+  KeyCodes<D> k;
+  ValueCodes<D> v;
+  float sk, sv;
+  bool there;
+};
+
+__device__ __forceinline__ void store_agent(float* p, float x, float y) {  // 8-byte device-scope store (p is 8-byte aligned)
+  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2v load_agent(const float* p) {
+  const unsigned long long u = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return float2v{__uint_as_float((unsigned)u), __uint_as_float((unsigned)(u >> 32))};
+}
+// factor of a part whose maximum is m in a sum under the maximum M
+__device__ __forceinline__ float part_factor(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
+
+// one row's result: channels c0 .. c0 + N - 1 (acc: sums under the total L), its logarithm from the thread of channel 0
+template <int D, bool BF, int N>
+__device__ __forceinline__ void write_row(const Args& a, int b, int h, int r, int c0, float M, float L, const float (&acc)[N]) {
+  const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;
+  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
+  alignas(16) uint16_t u[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) u[i] = from_float<BF>(acc[i] * inv);
+  if constexpr (N == 8)
+    *reinterpret_cast<uint4v*>(a.out + place * D + c0) = *reinterpret_cast<const uint4v*>(u);
+  else
+    *reinterpret_cast<uint2v*>(a.out + place * D + c0) = *reinterpret_cast<const uint2v*>(u);
+  if (c0 == 0) {
+    const float z = L == 0.f ? -INFINITY : M + __log2f(L);
+    if (a.lse) a.lse[place] = z * kLn2;
+    a.lse2[((int64_t)b * a.g.hkv + h) * a.rows + r] = z;
+  }
+}
 
 template <int D, int CODE, bool BF>
-__global__ __launch_bounds__(kWaves * 64) void rows_kernel(Args a) {
+__global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   constexpr int kCh = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), kg = lane >> 4, n = lane & 15;
   const int split = blockIdx.x % a.n_splits, unit = blockIdx.x / a.n_splits;
@@ -201,124 +249,228 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(Args a) {
   const int r0 = tile * 16, n_rows = pr.nq * a.g.ratio;
   if (r0 >= n_rows) return;
   const int r = r0 + n, last = min(r0 + 15, n_rows - 1);
-  const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : pr.len;
   const int vis_min = visible(a, pr, r0 / a.g.ratio), vis_max = visible(a, pr, last / a.g.ratio);
-  const int blk0 = split * a.per, blk1 = min(blk0 + a.per, (vis_max + kBlock - 1) / kBlock);
+  // the splits that hold a token (one at least: a tile of rows that see nothing is written too)
+  const int blocks = (vis_max + kBlock - 1) / kBlock, live = max(1, (blocks + a.per - 1) / a.per);
+  if (split >= live) return;
+  const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : pr.len;
+  const int blk0 = split * a.per, blk1 = min(blk0 + a.per, blocks);
+  const int64_t line0 = ((int64_t)b * a.g.hkv + h) * a.rows + r0;
 
+  auto fetch = [&](Fetched<D>& x, int blk) {  // (always loads: block 0 of the cache in the place of one that is not there)
+    int64_t pk = block_place(a.g, a.kc.block_table, b, h, blk), pv = block_place(a.g, a.vc.block_table, b, h, blk);
+    x.there = pk >= 0 && pv >= 0;
+    if (!x.there) pk = pv = 0;
+    x.k.load(a.kc.codes + pk * (int64_t)(kBlock * D));
+    x.v.load(a.vc.codes + pv * (int64_t)(kBlock * D));
+    x.sk = a.kc.scales[pk], x.sv = a.vc.scales[pv];
+  };
   half8v q[D / 32];
-  const float factor = load_queries<D, BF>(a, b, h, r, pr.nq, q);
-  float m = -INFINITY, l = 0.f;
+  float factor = 0.f, m = -INFINITY, l = 0.f;
   float4v o[kCh];
 #pragma unroll
   for (int i = 0; i < kCh; ++i) o[i] = float4v{0.f, 0.f, 0.f, 0.f};
 
-  for (int blk = blk0 + wave; blk < blk1; blk += kWaves) {
-    const int64_t pk = block_place(a.g, a.kc.block_table, b, h, blk), pv = block_place(a.g, a.vc.block_table, b, h, blk);
-    if (pk < 0 || pv < 0) continue;
-    KeyCodes<D> kw;
-    ValueCodes<D> vw;
-    kw.load(a.kc.codes + pk * (int64_t)(kBlock * D));
-    vw.load(a.vc.codes + pv * (int64_t)(kBlock * D));
-    const float f = factor * a.kc.scales[pk], sv = a.vc.scales[pv];
+  auto work = [&](Fetched<D>& x, int blk) {
     const int t0 = blk * kBlock;
-    if (CODE == NSN_Q8_E4M3 && t0 + kBlock > pr.len) vw.clear_from(pr.len - t0);
-
+    float* sc = a.scores ? a.scores + (line0 + n) * a.score_stride + t0 + 4 * kg : nullptr;
+    if (!x.there) {
+      if (sc && r < n_rows) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<float4v*>(sc + 16 * j) = float4v{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+      return;
+    }
+    if (CODE == NSN_Q8_E4M3 && t0 + kBlock > pr.len) x.v.clear_from(pr.len - t0);
+    const float f = factor * x.sk;
     float4v s[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       s[j] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < D / 32; ++ks)
-        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kw.template operand<CODE>(j, ks), q[ks], s[j], 0, 0, 0);
+        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.k.template operand<CODE>(j, ks), q[ks], s[j], 0, 0, 0);
     }
     float top = -INFINITY;
-    const bool masked = t0 + kBlock > vis_min;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] *= f;
+    if (t0 + kBlock > vis_min) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (t0 + 16 * j + 4 * kg + e >= vis) s[j][e] = -INFINITY;
+    }
+    if (sc && r < n_rows) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<float4v*>(sc + 16 * j) = s[j];
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[j][e] *= f;
-        if (masked && t0 + 16 * j + 4 * kg + e >= vis) s[j][e] = -INFINITY;
-        top = fmaxf(top, s[j][e]);
-      }
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, s[j][e]);
     top = fmaxf(top, __shfl_xor(top, 16, 64));
     top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = fast_exp2(m - base);
+    const float m_new = fmaxf(m, top), alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
+    const float base = m_new == -INFINITY ? 0.f : m_new - kRowsLift;
     m = m_new;
     l *= alpha;
     half8v p[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
+      float4v w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = fast_exp2(s[j][e] - base);
-        l += x;
-        p[j >> 1][4 * (j & 1) + e] = (_Float16)x;
+        w[e] = fast_exp2(s[j][e] - base);
+        l += w[e];
       }
+      const half4v u = __builtin_convertvector(w, half4v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[j >> 1][4 * (j & 1) + e] = u[e];
+    }
 #pragma unroll
     for (int c2 = 0; c2 < kCh / 2; ++c2) {
       float4v u = {0.f, 0.f, 0.f, 0.f}, v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        half8v x, y;
-        vw.template operands<CODE>(st, c2, x, y);
-        u = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, p[st], u, 0, 0, 0);
-        v = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, p[st], v, 0, 0, 0);
+        half8v y, z;
+        x.v.template operands<CODE>(st, c2, y, z);
+        u = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, p[st], u, 0, 0, 0);
+        v = __builtin_amdgcn_mfma_f32_16x16x32_f16(z, p[st], v, 0, 0, 0);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        o[2 * c2][e] = fmaf(sv, u[e], o[2 * c2][e] * alpha);
-        o[2 * c2 + 1][e] = fmaf(sv, v[e], o[2 * c2 + 1][e] * alpha);
+        o[2 * c2][e] = fmaf(x.sv, u[e], o[2 * c2][e] * alpha);
+        o[2 * c2 + 1][e] = fmaf(x.sv, v[e], o[2 * c2 + 1][e] * alpha);
       }
+    }
+  };
+  int blk = blk0 + wave;
+  if (blk < blk1) {
+    Fetched<D> x, y;
+    fetch(x, blk);
+    factor = load_queries<D, BF>(a, b, h, r, pr.nq, q);
+    while (true) {
+      fetch(y, min(blk + kWaves, blk1 - 1));
+      work(x, blk);
+      blk += kWaves;
+      if (blk >= blk1) break;
+      fetch(x, min(blk + kWaves, blk1 - 1));
+      work(y, blk);
+      blk += kWaves;
+      if (blk >= blk1) break;
     }
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
 
-  // join the four waves: row n of wave w, channels kCh * (4 kg + e) + i
-  constexpr int kStride = D + 4;  // (16-byte rows, the 16 rows of a wave on different banks)
-  __shared__ float sm_o[kWaves][16][kStride];
+  // join the four waves: row n of wave w, channels kCh * (4 kg + e) + i; sums under 2^(m - kRowsLift)
+  constexpr int kStride = D + 4;
+  __shared__ __attribute__((aligned(16))) float sm_o[kWaves][16][kStride];
   __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
-  if (kg == 0) sm_m[wave][n] = m, sm_l[wave][n] = l;
+  if (kg == 0) sm_m[wave][n] = m - kRowsLift, sm_l[wave][n] = l;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) sm_o[wave][n][kCh * (4 * kg + e) + i] = o[i][e];
+    for (int i = 0; i < kCh; i += 4)
+      *reinterpret_cast<float4v*>(&sm_o[wave][n][kCh * (4 * kg + e) + i]) = float4v{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]};
   __syncthreads();
-  // 16 threads per row, D / 16 channels each
-  const int row = tid >> 4, c0 = (tid & 15) * kCh;
-  if (r0 + row >= n_rows) return;
+  const int rows_here = min(16, n_rows - r0);
+  {
+    // 16 threads per row, D / 16 channels each
+    const int row = tid >> 4, c0 = (tid & 15) * kCh;
+    float M = -INFINITY, L = 0.f, acc[kCh];
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_m[w][row]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float e = part_factor(sm_m[w][row], M);
+      L = fmaf(e, sm_l[w][row], L);
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, sm_o[w][row][c0 + i], acc[i]);
+    }
+    if (live == 1) {
+      if (row < rows_here) write_row<D, BF, kCh>(a, b, h, r0 + row, c0, M, L, acc);
+      return;
+    }
+    if (row < rows_here) {
+      float* P = a.partial + ((line0 + row) * a.n_splits + split) * (D + 2);
+#pragma unroll
+      for (int i = 0; i < kCh; i += 2) store_agent(P + c0 + i, acc[i], acc[i + 1]);
+      if (c0 == 0) store_agent(P + D, M, L);
+    }
+  }
+  // The partials are device-scope stores (no cache holds them back); each wave waits until its own are acknowledged, then one
+  // thread counts the workgroup in, and the one that counts last reads all with device-scope loads.
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  __shared__ int arrived;
+  if (tid == 0) {
+    int* cnt = a.counters + ((b * a.row_tiles + tile) * a.g.hkv + h) * kCounterInts;
+    arrived = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (arrived == live - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
+  }
+  __syncthreads();
+  if (arrived != live - 1) return;
+  // groups of 16 threads take (row, every G-th split); few rows leave more groups per row, which are joined through LDS
+  int shift = 0;
+  while ((1 << shift) < rows_here) ++shift;
+  const int group = tid >> 4, row = group & ((1 << shift) - 1), g0 = group >> shift, G = 16 >> shift, c0 = (tid & 15) * kCh;
   float M = -INFINITY, L = 0.f, acc[kCh];
 #pragma unroll
   for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+  if (row < rows_here) {
+    const float* P = a.partial + (line0 + row) * a.n_splits * (D + 2);
+    constexpr int kAhead = 4;
+    for (int s0 = g0; s0 < live; s0 += kAhead * G) {
+      float2v ml[kAhead], x[kAhead][kCh / 2];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_m[w][row]);
+      for (int k = 0; k < kAhead; ++k) {
+        const float* ps = P + (int64_t)min(s0 + k * G, live - 1) * (D + 2);
+        ml[k] = load_agent(ps + D);
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float e = sm_m[w][row] == -INFINITY && M == -INFINITY ? 0.f : fast_exp2(sm_m[w][row] - M);
-    L = fmaf(e, sm_l[w][row], L);
+        for (int i = 0; i < kCh / 2; ++i) x[k][i] = load_agent(ps + c0 + 2 * i);
+      }
+      float m2 = M;
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, sm_o[w][row][c0 + i], acc[i]);
+      for (int k = 0; k < kAhead; ++k)
+        if (s0 + k * G < live) m2 = fmaxf(m2, ml[k][0]);
+      const float turn = part_factor(M, m2);
+      M = m2;
+      L *= turn;
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] *= turn;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float e = s0 + k * G < live ? part_factor(ml[k][0], M) : 0.f;
+        L = fmaf(e, ml[k][1], L);
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, x[k][i / 2][i & 1], acc[i]);
+      }
+    }
   }
-  const int64_t line = ((int64_t)b * a.g.hkv + h) * a.rows + r0 + row;
-  if (a.n_splits > 1) {
-    float* P = a.partial + (line * a.n_splits + split) * (D + 2);
+  float* flat = &sm_o[0][0][0];
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) P[c0 + i] = acc[i];
-    if (c0 == 0) P[D] = M, P[D + 1] = L;
-    return;
-  }
-  const int i_q = (r0 + row) / a.g.ratio, hq = h * a.g.ratio + (r0 + row) % a.g.ratio;
-  const int64_t place = ((int64_t)b * a.n_q + i_q) * a.g.hq + hq;
-  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
+  for (int i = 0; i < kCh; ++i) flat[group * kStride + c0 + i] = acc[i];
+  float* mls = &sm_m[0][0];  // [group]: M; sm_l: L
+  if (c0 == 0) mls[group] = M, (&sm_l[0][0])[group] = L;
+  __syncthreads();
+  if (g0 != 0 || row >= rows_here) return;
+  float Mt = -INFINITY;
+  for (int k = 0; k < G; ++k) Mt = fmaxf(Mt, mls[(k << shift) + row]);
+  L = 0.f;
 #pragma unroll
-  for (int i = 0; i < kCh; ++i) a.out[place * D + c0 + i] = from_float<BF>(acc[i] * inv);
-  if (c0 == 0) {
-    const float z = L == 0.f ? -INFINITY : M + __log2f(L);
-    if (a.lse) a.lse[place] = z * kLn2;
-    if (a.lse2) a.lse2[line] = z;
+  for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+  for (int k = 0; k < G; ++k) {
+    const int at = (k << shift) + row;
+    const float e = part_factor(mls[at], Mt);
+    L = fmaf(e, (&sm_l[0][0])[at], L);
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, flat[at * kStride + c0 + i], acc[i]);
   }
+  write_row<D, BF, kCh>(a, b, h, r0 + row, c0, Mt, L, acc);
 }
 
 // ---- many rows: tiles in LDS ------------------------------------------------------------------------------
@@ -552,12 +704,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     } else {
       const float z = l == 0.f ? -INFINITY : M + __log2f(l);
       if (a.lse) a.lse[place] = z * kLn2;
-      if (a.lse2) a.lse2[line] = z;
+      a.lse2[line] = z;
     }
   }
 }
 
-// the splits of a row are joined: one workgroup of D threads per row
+// the splits of a chunk's rows are joined: one workgroup of D threads per row
 template <int D, bool BF>
 __global__ __launch_bounds__(D) void merge_kernel(Args a) {
   const int r = blockIdx.x / a.g.hkv, h = blockIdx.x % a.g.hkv, b = blockIdx.y, c = threadIdx.x;
@@ -569,7 +721,7 @@ __global__ __launch_bounds__(D) void merge_kernel(Args a) {
   for (int s = 0; s < a.n_splits; ++s) M = fmaxf(M, P[s * (D + 2) + D]);
   for (int s = 0; s < a.n_splits; ++s) {
     const float ms = P[s * (D + 2) + D];
-    const float e = ms == -INFINITY && M == -INFINITY ? 0.f : fast_exp2(ms - M);
+    const float e = part_factor(ms, M);
     L = fmaf(e, P[s * (D + 2) + D + 1], L);
     acc = fmaf(e, P[s * (D + 2) + c], acc);
   }
@@ -579,7 +731,7 @@ __global__ __launch_bounds__(D) void merge_kernel(Args a) {
   if (c == 0) {
     const float z = L == 0.f ? -INFINITY : M + __log2f(L);
     if (a.lse) a.lse[place] = z * kLn2;
-    if (a.lse2) a.lse2[line] = z;
+    a.lse2[line] = z;
   }
 }
 
@@ -635,33 +787,73 @@ __global__ __launch_bounds__(kWaves * 64) void weights_kernel(Args a) {
   }
 }
 
+// The same from the scores that a call of few rows has left behind: a thread takes four tokens and goes through the rows.
+constexpr int kScoreThreads = 256;
+__global__ __launch_bounds__(kScoreThreads) void weights_of_scores_kernel(Args a) {
+  const int h = blockIdx.y, b = blockIdx.z;
+  const Problem pr = problem_of(a, b);
+  const int t = (blockIdx.x * kScoreThreads + threadIdx.x) * 4, n_rows = pr.nq * a.g.ratio;
+  if (t >= pr.len) return;
+  const int64_t line0 = ((int64_t)b * a.g.hkv + h) * a.rows;
+  float4v x = {0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < n_rows; ++r) {
+    // (a row's scores end with the block of the last token that its tile of rows sees)
+    if (t >= (visible(a, pr, min(r | 15, n_rows - 1) / a.g.ratio) + kBlock - 1) / kBlock * kBlock) continue;
+    const float4v s = *reinterpret_cast<const float4v*>(a.scores + (line0 + r) * a.score_stride + t);
+    const float z = a.lse2[line0 + r];
+    if (z == -INFINITY) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += fast_exp2(s[e] - z);
+  }
+  const int64_t at = ((int64_t)b * a.g.hkv + h) * a.g.max_len + t;
+  for (int e = 0; e < min(4, pr.len - t); ++e) a.weights_out[at + e] = a.weights_in ? a.weights_in[at + e] + x[e] : x[e];
+}
+
 // ---- host side --------------------------------------------------------------------------------------------
 // from this many rows of a (sequence, kv head) on, tiles in LDS
 static bool use_chunk(int64_t rows) { return rows > 32; }
 
-static int split_count(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int requested) {
-  const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
-  if (requested > 0) return std::min(requested, blocks);
-  const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads);
-  if (use_chunk(rows)) {
-    const int64_t groups = (rows + 32 * kWaves - 1) / (32 * kWaves) * s.n_kv_heads * batch;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, 512 / groups));
-  }
-  const int64_t groups = (rows + 15) / 16 * s.n_kv_heads * batch, most = (blocks + kWaves - 1) / kWaves;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, 1024 / groups));
-}
-
-static int64_t lines(const nsn_q8_shape& s, int batch, int n_q) { return (int64_t)batch * n_q * s.n_q_heads; }
 static size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
-size_t attention_workspace_bytes(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int n_splits) {
-  const int splits = split_count(s, batch, n_q, max_seq_len, n_splits);
-  const size_t rows = (size_t)lines(s, batch, n_q);
-  return up16(rows * sizeof(float)) + (splits > 1 ? rows * splits * (s.head_dim + 2) * sizeof(float) : 0);
+// How a call is cut, and where its workspace's parts lie
+struct Plan {
+  bool chunk;
+  int64_t tiles;  // of rows
+  int splits, per;
+  bool scores;
+  size_t lse2_at, partial_at, scores_at, bytes;
+  int64_t score_stride;
+};
+static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int requested, bool weights) {
+  Plan p;
+  const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads), lines = rows * s.n_kv_heads * batch;
+  p.chunk = use_chunk(rows);
+  const int per_tile = p.chunk ? 32 * kWaves : 16;
+  p.tiles = (rows + per_tile - 1) / per_tile;
+  const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
+  const int64_t groups = p.tiles * s.n_kv_heads * batch;
+  int64_t splits = requested;
+  if (requested <= 0) splits = p.chunk ? std::min<int64_t>((blocks + 7) / 8, 512 / groups) : std::min<int64_t>((blocks + 15) / 16, 2048 / groups);
+  if (!p.chunk && groups > kMaxCounters) splits = 1;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, blocks));
+  p.per = (blocks + p.splits - 1) / p.splits;
+  p.scores = weights && rows <= 16;
+  p.score_stride = (int64_t)blocks * kBlock;
+  p.lse2_at = (size_t)kMaxCounters * kCounterInts * sizeof(int);
+  p.partial_at = p.lse2_at + up16(lines * sizeof(float));
+  p.scores_at = p.partial_at + (p.splits > 1 ? up16((size_t)lines * p.splits * (s.head_dim + 2) * sizeof(float)) : 0);
+  p.bytes = p.scores_at + (p.scores ? (size_t)lines * p.score_stride * sizeof(float) : 0);
+  return p;
+}
+
+size_t attention_workspace_bytes(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int n_splits, bool weights) {
+  return plan_of(s, batch, n_q, max_seq_len, n_splits, weights).bytes;
 }
 
 int attention_launch(const AttentionCall& c) {
   const nsn_q8_shape& s = c.shape;
+  const Plan plan = plan_of(s, c.batch, c.n_q, c.max_seq_len, c.n_splits, c.weights_out != nullptr);
+  unsigned char* ws = static_cast<unsigned char*>(c.workspace);
   Args a;
   a.g = make_geometry(s);
   a.q = make_rows(c.q);
@@ -669,33 +861,38 @@ int attention_launch(const AttentionCall& c) {
   a.kc = make_view(c.kc), a.vc = make_view(c.vc);
   a.seq_lens = c.seq_lens, a.max_seq_len = c.max_seq_len;
   a.scale_log2 = c.scale * kLog2e, a.causal = c.causal;
-  a.n_splits = split_count(s, c.batch, c.n_q, c.max_seq_len, c.n_splits);
-  const int blocks = std::max(1, (c.max_seq_len + kBlock - 1) / kBlock);
-  a.per = (blocks + a.n_splits - 1) / a.n_splits;
+  a.n_splits = plan.splits, a.per = plan.per;
   a.out = static_cast<uint16_t*>(c.out), a.lse = c.lse;
-  a.lse2 = static_cast<float*>(c.workspace);
-  a.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(c.workspace) + up16(lines(s, c.batch, c.n_q) * sizeof(float)));
+  a.counters = reinterpret_cast<int*>(ws);
+  a.row_tiles = (int)plan.tiles;
+  a.lse2 = reinterpret_cast<float*>(ws + plan.lse2_at);
+  a.partial = reinterpret_cast<float*>(ws + plan.partial_at);
+  a.scores = plan.scores ? reinterpret_cast<float*>(ws + plan.scores_at) : nullptr;
+  a.score_stride = plan.score_stride;
   a.weights_in = c.weights_in, a.weights_out = c.weights_out;
   return with_types(s, [&](auto d, auto code, auto bf) -> int {
     constexpr int D = decltype(d)::value, CODE = decltype(code)::value;
     constexpr bool BF = decltype(bf)::value;
-    const bool chunk = use_chunk(a.rows);
-    const int tiles = chunk ? (a.rows + 32 * kWaves - 1) / (32 * kWaves) : (a.rows + 15) / 16;
-    if ((int64_t)tiles * a.g.hkv * a.n_splits > 0x7fffffff || (int64_t)a.rows * a.g.hkv > 0x7fffffff) {
+    const int64_t groups = plan.tiles * a.g.hkv * plan.splits;
+    if (groups > 0x7fffffff || (int64_t)a.rows * a.g.hkv > 0x7fffffff) {
       set_error("q8_attention: n_q * n_q_heads * n_splits is too large for one launch");
       return NSN_ERR_UNSUPPORTED;
     }
-    if (chunk)
-      chunk_kernel<D, CODE, BF><<<dim3(tiles * a.g.hkv * a.n_splits, c.batch), kWaves * 64, 0, c.stream>>>(a);
+    const dim3 grid((unsigned)groups, c.batch);
+    if (plan.chunk)
+      chunk_kernel<D, CODE, BF><<<grid, kWaves * 64, 0, c.stream>>>(a);
     else
-      rows_kernel<D, CODE, BF><<<dim3(tiles * a.g.hkv * a.n_splits, c.batch), kWaves * 64, 0, c.stream>>>(a);
+      rows_kernel<D, CODE, BF><<<grid, kWaves * 64, 0, c.stream>>>(a);
     if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
-    if (a.n_splits > 1) {
+    if (plan.chunk && plan.splits > 1) {
       merge_kernel<D, BF><<<dim3(a.rows * a.g.hkv, c.batch), D, 0, c.stream>>>(a);
       if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
     }
     if (a.weights_out && c.max_seq_len > 0) {
-      weights_kernel<D, CODE, BF><<<dim3(blocks, a.g.hkv, c.batch), kWaves * 64, 0, c.stream>>>(a);
+      if (plan.scores)
+        weights_of_scores_kernel<<<dim3((c.max_seq_len + 4 * kScoreThreads - 1) / (4 * kScoreThreads), a.g.hkv, c.batch), kScoreThreads, 0, c.stream>>>(a);
+      else
+        weights_kernel<D, CODE, BF><<<dim3((c.max_seq_len + kBlock - 1) / kBlock, a.g.hkv, c.batch), kWaves * 64, 0, c.stream>>>(a);
       if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
     }
     return NSN_OK;

@@ -31,12 +31,13 @@ struct Args {
   int max_seq_len;
   float scale_log2;  // softmax_scale * log2 e
   int causal;
-  int n_splits, per;  // per: blocks of a split
+  int batch;
+  int n_splits, per;  // chunks: splits and their blocks; few rows: runs, and the fewest blocks of one
   uint16_t* out;
   float* lse;
   float* lse2;     // [batch][hkv][rows], in powers of two (workspace)
-  float* partial;  // [batch][hkv][rows][split][D + 2] (workspace)
-  int* counters;   // [batch][row tile][hkv], one per 64 bytes: splits that have arrived (workspace)
+  float* partial;  // chunks: [batch][hkv][rows][split][D + 2]; few rows: [run][2][16][D + 2] (workspace)
+  int* counters;   // of the unit that goes on behind a run, one per 64 bytes: runs that have arrived (workspace)
   int row_tiles;
   float* scores;   // [batch][hkv][rows][score_stride] in powers of two, -infinity where nothing is seen (workspace), or NULL
   int64_t score_stride;
@@ -195,11 +196,41 @@ struct ValueCodes {
 };
 
 // ---- few rows: the token axis is split -------------------------------------------------------------------
-// One workgroup of four waves per (16 rows, split); the waves take the split's blocks in turn, each with the next block's codes on
-// their way to registers while it works on one, and are joined through LDS.  The splits of a tile of rows are joined by the last
-// workgroup that arrives.  Bound by memory: every code is read once, and the conversions and products of a block fill a
-// third of the time that its bytes take.
+// The work is the list of all 64-token blocks of all units (16 rows of a (sequence, kv head)), cut into equal runs of one workgroup
+// each, whatever the sequences' lengths: with two workgroups to a compute unit all of them end at about the same time, where a grid
+// over (unit, split) leaves a last round that few take part in.  A run is a few segments, each of one unit.  The four waves of a
+// workgroup take a segment's blocks in turn, each with the next block's codes on their way to registers while it works on
+// one, and are joined through LDS; the segments of a unit that reaches into other runs are joined by the last workgroup that
+// arrives.  Bound by memory: every code is read once, and the conversions and products of a block fill a third of the time that its
+// bytes take.
 constexpr int kRowsLift = 12;  // weights are 2^kRowsLift at most: those down to 2^-26 of the largest are normal fp16 numbers
+
+// what a unit counts in the list: its blocks, and one where its rows see nothing (they are written too); no rows: nothing
+__device__ __forceinline__ int unit_cost(const Args& a, const Problem& p, int tile) {
+  const int n_rows = p.nq * a.g.ratio;
+  if (tile * 16 >= n_rows) return 0;
+  return max(1, (visible(a, p, min(tile * 16 + 15, n_rows - 1) / a.g.ratio) + kBlock - 1) / kBlock);
+}
+__device__ __forceinline__ int sequence_cost(const Args& a, int b) {
+  const Problem p = problem_of(a, b);
+  int c = 0;
+  for (int tile = 0; tile < a.row_tiles; ++tile) c += unit_cost(a, p, tile);
+  return c * a.g.hkv;
+}
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_prefix_sum(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int o = __shfl_up(v, m, 64);
+    if (lane >= m) v += o;
+  }
+  return v;
+}
 
 template <int D>
 struct Fetched {
@@ -243,18 +274,42 @@ template <int D, int CODE, bool BF>
 __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   constexpr int kCh = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), kg = lane >> 4, n = lane & 15;
-  const int split = blockIdx.x % a.n_splits, unit = blockIdx.x / a.n_splits;
-  const int h = unit % a.g.hkv, tile = unit / a.g.hkv, b = blockIdx.y;
-  const Problem pr = problem_of(a, b);
-  const int r0 = tile * 16, n_rows = pr.nq * a.g.ratio;
-  if (r0 >= n_rows) return;
-  const int r = r0 + n, last = min(r0 + 15, n_rows - 1);
-  const int vis_min = visible(a, pr, r0 / a.g.ratio), vis_max = visible(a, pr, last / a.g.ratio);
-  // the splits that hold a token (one at least: a tile of rows that see nothing is written too)
-  const int blocks = (vis_max + kBlock - 1) / kBlock, live = max(1, (blocks + a.per - 1) / a.per);
-  if (split >= live) return;
+  // the whole list's length, and the unit in which this run begins
+  const int run = blockIdx.x;
+  int total = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) total += wave_sum(b0 + lane < a.batch ? sequence_cost(a, b0 + lane) : 0);
+  const int per = max(a.per, (total + a.n_splits - 1) / a.n_splits);
+  if (run * per >= total) return;  // (also where no sequence has a query)
+  int pos = run * per, b = 0, at = 0;  // at: where sequence b begins
+  const int end = min(pos + per, total);
+  for (int b0 = 0, before = 0; b0 < a.batch; b0 += 64) {
+    const int cost = b0 + lane < a.batch ? sequence_cost(a, b0 + lane) : 0, upto = before + wave_prefix_sum(cost);
+    const unsigned long long found = __ballot(pos < upto);
+    if (found) {
+      const int k = __ffsll(found) - 1;
+      b = b0 + k, at = __builtin_amdgcn_readlane(upto - cost, k);
+      break;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  constexpr int kStride = D + 4;
+  __shared__ __attribute__((aligned(16))) float sm_o[kWaves][16][kStride];
+  __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
+  __shared__ int arrived;
+  Problem pr = problem_of(a, b);
+  int tile = 0, h = 0;
+  for (int c; at + (c = unit_cost(a, pr, tile) * a.g.hkv) <= pos; ++tile) at += c;
+  {
+    const int c = unit_cost(a, pr, tile);
+    h = (pos - at) / c;
+    at += h * c;  // where the unit begins
+  }
+  while (true) {  // segments
+  const int cost = unit_cost(a, pr, tile), n_rows = pr.nq * a.g.ratio, r0 = tile * 16, r = r0 + n;
+  const int vis_min = visible(a, pr, r0 / a.g.ratio), blocks = (visible(a, pr, min(r0 + 15, n_rows - 1) / a.g.ratio) + kBlock - 1) / kBlock;
   const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : pr.len;
-  const int blk0 = split * a.per, blk1 = min(blk0 + a.per, blocks);
+  const int blk0 = pos - at, blk1 = min(min(blocks, cost), blk0 + end - pos);
+  const int first_run = at / per, live = (at + cost - 1) / per - first_run + 1;  // the runs that the unit reaches into
   const int64_t line0 = ((int64_t)b * a.g.hkv + h) * a.rows + r0;
 
   auto fetch = [&](Fetched<D>& x, int blk) {  // (always loads: block 0 of the cache in the place of one that is not there)
@@ -365,9 +420,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   l += __shfl_xor(l, 32, 64);
 
   // join the four waves: row n of wave w, channels kCh * (4 kg + e) + i; sums under 2^(m - kRowsLift)
-  constexpr int kStride = D + 4;
-  __shared__ __attribute__((aligned(16))) float sm_o[kWaves][16][kStride];
-  __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
   if (kg == 0) sm_m[wave][n] = m - kRowsLift, sm_l[wave][n] = l;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -376,6 +428,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       *reinterpret_cast<float4v*>(&sm_o[wave][n][kCh * (4 * kg + e) + i]) = float4v{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]};
   __syncthreads();
   const int rows_here = min(16, n_rows - r0);
+  // the partial of the unit's k-th run: a run has room for two, one of a unit that began before it and one of a unit that
+  // begins in it and goes on behind it
+  auto partial_of = [&](int k) { return a.partial + ((int64_t)(first_run + k) * 2 + (k == 0)) * 16 * (D + 2); };
+  [&] {
   {
     // 16 threads per row, D / 16 channels each
     const int row = tid >> 4, c0 = (tid & 15) * kCh;
@@ -396,7 +452,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       return;
     }
     if (row < rows_here) {
-      float* P = a.partial + ((line0 + row) * a.n_splits + split) * (D + 2);
+      float* P = partial_of(run - first_run) + row * (D + 2);
 #pragma unroll
       for (int i = 0; i < kCh; i += 2) store_agent(P + c0 + i, acc[i], acc[i + 1]);
       if (c0 == 0) store_agent(P + D, M, L);
@@ -406,9 +462,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   // thread counts the workgroup in, and the one that counts last reads all with device-scope loads.
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  __shared__ int arrived;
   if (tid == 0) {
-    int* cnt = a.counters + ((b * a.row_tiles + tile) * a.g.hkv + h) * kCounterInts;
+    int* cnt = a.counters + first_run * kCounterInts;
     arrived = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (arrived == live - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
   }
@@ -422,13 +477,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
 #pragma unroll
   for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
   if (row < rows_here) {
-    const float* P = a.partial + (line0 + row) * a.n_splits * (D + 2);
     constexpr int kAhead = 4;
     for (int s0 = g0; s0 < live; s0 += kAhead * G) {
       float2v ml[kAhead], x[kAhead][kCh / 2];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const float* ps = P + (int64_t)min(s0 + k * G, live - 1) * (D + 2);
+        const float* ps = partial_of(min(s0 + k * G, live - 1)) + row * (D + 2);
         ml[k] = load_agent(ps + D);
 #pragma unroll
         for (int i = 0; i < kCh / 2; ++i) x[k][i] = load_agent(ps + c0 + 2 * i);
@@ -471,6 +525,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
     for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, flat[at * kStride + c0 + i], acc[i]);
   }
   write_row<D, BF, kCh>(a, b, h, r0 + row, c0, Mt, L, acc);
+  }();
+  pos += min(cost - blk0, end - pos);
+  if (pos >= end) break;
+  // the next unit (one with rows: pos < total)
+  at = pos;
+  if (++h == a.g.hkv) {
+    h = 0, ++tile;
+    while (unit_cost(a, pr, tile) == 0) pr = problem_of(a, ++b), tile = 0;
+  }
+  __syncthreads();  // the joining has left LDS
+  }
 }
 
 // ---- many rows: tiles in LDS ------------------------------------------------------------------------------
@@ -832,16 +897,25 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   p.tiles = (rows + per_tile - 1) / per_tile;
   const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
   const int64_t groups = p.tiles * s.n_kv_heads * batch;
-  int64_t splits = requested;
-  if (requested <= 0) splits = p.chunk ? std::min<int64_t>((blocks + 7) / 8, 512 / groups) : std::min<int64_t>((blocks + 15) / 16, 2048 / groups);
-  if (!p.chunk && groups > kMaxCounters) splits = 1;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, blocks));
-  p.per = (blocks + p.splits - 1) / p.splits;
+  size_t partials = 0;
+  if (p.chunk) {
+    const int64_t splits = requested > 0 ? requested : std::min<int64_t>((blocks + 7) / 8, 512 / groups);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, blocks));
+    p.per = (blocks + p.splits - 1) / p.splits;
+    if (p.splits > 1) partials = (size_t)lines * p.splits;
+  } else {
+    // runs: two workgroups to each of the 256 compute units, or one per unit where there are more; four blocks at least (a wave
+    // each), as a run's start and joining take as long as some blocks
+    p.per = requested > 0 ? 1 : kWaves;
+    const int64_t runs = requested > 0 ? requested * groups : std::max<int64_t>(512, groups);
+    p.splits = (int)std::min<int64_t>(std::min<int64_t>(runs, kMaxCounters), (groups * blocks + p.per - 1) / p.per);
+    partials = (size_t)p.splits * 2 * 16;
+  }
   p.scores = weights && rows <= 16;
   p.score_stride = (int64_t)blocks * kBlock;
   p.lse2_at = (size_t)kMaxCounters * kCounterInts * sizeof(int);
   p.partial_at = p.lse2_at + up16(lines * sizeof(float));
-  p.scores_at = p.partial_at + (p.splits > 1 ? up16((size_t)lines * p.splits * (s.head_dim + 2) * sizeof(float)) : 0);
+  p.scores_at = p.partial_at + up16(partials * (s.head_dim + 2) * sizeof(float));
   p.bytes = p.scores_at + (p.scores ? (size_t)lines * p.score_stride * sizeof(float) : 0);
   return p;
 }
@@ -861,7 +935,7 @@ int attention_launch(const AttentionCall& c) {
   a.kc = make_view(c.kc), a.vc = make_view(c.vc);
   a.seq_lens = c.seq_lens, a.max_seq_len = c.max_seq_len;
   a.scale_log2 = c.scale * kLog2e, a.causal = c.causal;
-  a.n_splits = plan.splits, a.per = plan.per;
+  a.batch = c.batch, a.n_splits = plan.splits, a.per = plan.per;
   a.out = static_cast<uint16_t*>(c.out), a.lse = c.lse;
   a.counters = reinterpret_cast<int*>(ws);
   a.row_tiles = (int)plan.tiles;
@@ -873,16 +947,15 @@ int attention_launch(const AttentionCall& c) {
   return with_types(s, [&](auto d, auto code, auto bf) -> int {
     constexpr int D = decltype(d)::value, CODE = decltype(code)::value;
     constexpr bool BF = decltype(bf)::value;
-    const int64_t groups = plan.tiles * a.g.hkv * plan.splits;
-    if (groups > 0x7fffffff || (int64_t)a.rows * a.g.hkv > 0x7fffffff) {
-      set_error("q8_attention: n_q * n_q_heads * n_splits is too large for one launch");
+    const int64_t groups = plan.tiles * a.g.hkv * plan.splits, listed = plan.tiles * a.g.hkv * c.batch * (a.score_stride / kBlock);
+    if (plan.chunk ? groups > 0x7fffffff || (int64_t)a.rows * a.g.hkv > 0x7fffffff : listed > 0x3fffffff) {
+      set_error("q8_attention: batch * n_q * n_q_heads * max_seq_len is too large for one launch");
       return NSN_ERR_UNSUPPORTED;
     }
-    const dim3 grid((unsigned)groups, c.batch);
     if (plan.chunk)
-      chunk_kernel<D, CODE, BF><<<grid, kWaves * 64, 0, c.stream>>>(a);
+      chunk_kernel<D, CODE, BF><<<dim3((unsigned)groups, c.batch), kWaves * 64, 0, c.stream>>>(a);
     else
-      rows_kernel<D, CODE, BF><<<grid, kWaves * 64, 0, c.stream>>>(a);
+      rows_kernel<D, CODE, BF><<<plan.splits, kWaves * 64, 0, c.stream>>>(a);
     if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
     if (plan.chunk && plan.splits > 1) {
       merge_kernel<D, BF><<<dim3(a.rows * a.g.hkv, c.batch), D, 0, c.stream>>>(a);

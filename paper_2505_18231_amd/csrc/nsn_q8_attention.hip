@@ -655,13 +655,22 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
       const ChunkTile<D>& tl = sm[buf];
       float16v s[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
           s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8v*>(&tl.k[32 * j + n][16 * ks + 8 * hh]), q[ks], s[j], 0, 0, 0);
+      // (six operands asked for ahead of the first product, then one per product: LDS answers in about three products' time)
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < D / 8 - 6; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
+      __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
       const float f = factor * sk;
       const bool masked = t0 + kBlock > vis_min;
       if (masked) {

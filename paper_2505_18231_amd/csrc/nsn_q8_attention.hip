@@ -32,11 +32,12 @@ struct Args {
   float scale_log2;  // softmax_scale * log2 e
   int causal;
   int batch;
-  int n_splits, per;  // chunks: splits and their blocks; few rows: runs, and the fewest blocks of one
+  int n_runs, per;  // runs, and the fewest blocks of one
+  int direct;       // instead: a unit to each workgroup
   uint16_t* out;
   float* lse;
   float* lse2;     // [batch][hkv][rows], in powers of two (workspace)
-  float* partial;  // chunks: [batch][hkv][rows][split][D + 2]; few rows: [run][2][16][D + 2] (workspace)
+  float* partial;  // [run][2][a tile's sums] (workspace)
   int* counters;   // of the unit that goes on behind a run, one per 64 bytes: runs that have arrived (workspace)
   int row_tiles;
   float* scores;   // [batch][hkv][rows][score_stride] in powers of two, -infinity where nothing is seen (workspace), or NULL
@@ -195,42 +196,11 @@ struct ValueCodes {
   }
 };
 
-// ---- few rows: the token axis is split -------------------------------------------------------------------
-// The work is the list of all 64-token blocks of all units (16 rows of a (sequence, kv head)), cut into equal runs of one workgroup
-// each, whatever the sequences' lengths: with two workgroups to a compute unit all of them end at about the same time, where a grid
-// over (unit, split) leaves a last round that few take part in.  A run is a few segments, each of one unit.  The four waves of a
-// workgroup take a segment's blocks in turn, each with the next block's codes on their way to registers while it works on
-// one, and are joined through LDS; the segments of a unit that reaches into other runs are joined by the last workgroup that
-// arrives.  Bound by memory: every code is read once, and the conversions and products of a block fill a third of the time that its
-// bytes take.
+// ---- few rows -------------------------------------------------------------------
+// Units of 16 rows.  The four waves of a workgroup take a segment's blocks in turn, each with the next block's codes on their way
+// to registers while it works on one, and are joined through LDS.  Bound by memory: every code is read once, and the
+// conversions and products of a block fill a third of the time that its bytes take.
 constexpr int kRowsLift = 12;  // weights are 2^kRowsLift at most: those down to 2^-26 of the largest are normal fp16 numbers
-
-// what a unit counts in the list: its blocks, and one where its rows see nothing (they are written too); no rows: nothing
-__device__ __forceinline__ int unit_cost(const Args& a, const Problem& p, int tile) {
-  const int n_rows = p.nq * a.g.ratio;
-  if (tile * 16 >= n_rows) return 0;
-  return max(1, (visible(a, p, min(tile * 16 + 15, n_rows - 1) / a.g.ratio) + kBlock - 1) / kBlock);
-}
-__device__ __forceinline__ int sequence_cost(const Args& a, int b) {
-  const Problem p = problem_of(a, b);
-  int c = 0;
-  for (int tile = 0; tile < a.row_tiles; ++tile) c += unit_cost(a, p, tile);
-  return c * a.g.hkv;
-}
-__device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
-  return __builtin_amdgcn_readfirstlane(v);
-}
-__device__ __forceinline__ int wave_prefix_sum(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(v, m, 64);
-    if (lane >= m) v += o;
-  }
-  return v;
-}
 
 template <int D>
 struct Fetched {
@@ -240,6 +210,119 @@ struct Fetched {
   bool there;
 };
 
+// ---- the list of the work --------------------------------------------------------------------------------
+// A unit is a tile of TILE rows of a (sequence, kv head); the list holds the 64-token blocks of all units in the order (sequence,
+// head, tile).  It is cut into equal runs, one workgroup each, whatever the sequences' lengths: all workgroups end at about
+// the same time, where a grid over units and splits leaves a last round that few take part in.  A run is a few segments, each of one
+// unit.  A unit that reaches into other runs leaves partial sums, which the last workgroup to arrive joins.
+__device__ __forceinline__ int wave_scan(int v) {  // inclusive prefix sum over the 64 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row 0's and 2's last lane to the rows behind them
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the lower half's last lane to the upper half
+  return v;
+}
+
+template <int TILE>
+struct Cursor {
+  int b, h, tile, cost;  // the unit, and its blocks in the list
+  Problem pr;
+  int run, per, at, pos, end;  // at: where the unit begins; pos, end: what is left of the run
+
+  // a unit's blocks, and one where its rows see nothing (they are written too); no rows: nothing
+  static __device__ __forceinline__ int cost_of(const Args& a, const Problem& p, int tile) {
+    const int n_rows = p.nq * a.g.ratio;
+    if (tile * TILE >= n_rows) return 0;
+    return max(1, (visible(a, p, min(tile * TILE + TILE - 1, n_rows - 1) / a.g.ratio) + kBlock - 1) / kBlock);
+  }
+  // 64 / K sequences from b0 on, K lanes to each: what a lane's tiles of one head come to
+  static __device__ __forceinline__ int lane_cost(const Args& a, int b, int j, int K) {
+    if (b >= a.batch) return 0;
+    const Problem p = problem_of(a, b);
+    if (!a.causal) return j == 0 ? (p.nq * a.g.ratio + TILE - 1) / TILE * cost_of(a, p, 0) : 0;
+    int c = 0;
+    for (int t = j; t < a.row_tiles; t += K) c += cost_of(a, p, t);
+    return c;
+  }
+
+  // the run of this workgroup; false: there is none
+  __device__ __forceinline__ bool begin(const Args& a, int index) {
+    const int lane = threadIdx.x & 63;
+    run = index;
+    if (a.direct) {  // more units than runs could be useful: one to each workgroup, the last tiles (the longest) first
+      h = index % a.g.hkv;
+      const int item = index / a.g.hkv;
+      b = item % a.batch, tile = a.row_tiles - 1 - item / a.batch;
+      pr = problem_of(a, b);
+      cost = cost_of(a, pr, tile);
+      at = pos = 0, per = end = max(cost, 1), run = 0;
+      return cost > 0;
+    }
+    int shift = 0;  // K = 1 << shift lanes to a sequence
+    while ((a.batch << (shift + 1)) <= 64) ++shift;
+    const int K = 1 << shift, step = 64 >> shift;
+    int scan = 0, total = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += step) {
+      scan = wave_scan(lane_cost(a, b0 + (lane >> shift), lane & (K - 1), K));
+      total += __builtin_amdgcn_readlane(scan, 63);
+    }
+    total *= a.g.hkv;
+    per = max(a.per, (total + a.n_runs - 1) / a.n_runs);
+    pos = run * per;
+    if (pos >= total) return false;  // (also where no sequence has a query)
+    end = min(pos + per, total);
+    int before = 0;  // one head's blocks of the sequences before
+    for (int b0 = 0;; b0 += step) {
+      if (a.batch > step) scan = wave_scan(lane_cost(a, b0 + (lane >> shift), lane & (K - 1), K));
+      const unsigned long long found = __ballot((lane & (K - 1)) == K - 1 && (before + scan) * a.g.hkv > pos);
+      if (found) {
+        const int k = __ffsll(found) - 1;  // the last lane of the sequence
+        b = b0 + (k >> shift);
+        const int upto = __builtin_amdgcn_readlane(scan, k), from = k >= K ? __builtin_amdgcn_readlane(scan, k - K) : 0;
+        at = (before + from) * a.g.hkv;
+        h = (pos - at) / (upto - from);
+        at += h * (upto - from);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(scan, 63);
+    }
+    pr = problem_of(a, b);
+    for (int t0 = 0;; t0 += 64) {
+      const int c = cost_of(a, pr, t0 + lane), upto = wave_scan(c);
+      const unsigned long long found = __ballot(at + upto > pos);
+      if (found) {
+        const int k = __ffsll(found) - 1;
+        tile = t0 + k, cost = __builtin_amdgcn_readlane(c, k);
+        at += __builtin_amdgcn_readlane(upto, k) - cost;
+        break;
+      }
+      at += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return true;
+  }
+  // blocks of the unit that belong to this run: [first, last)
+  __device__ __forceinline__ int first() const { return pos - at; }
+  __device__ __forceinline__ int last() const { return min(cost, end - at); }
+  // the runs that the unit reaches into
+  __device__ __forceinline__ int first_run() const { return at / per; }
+  __device__ __forceinline__ int runs() const { return (at + cost - 1) / per - at / per + 1; }
+  // the next unit of the run; false: the run is done
+  __device__ __forceinline__ bool next(const Args& a) {
+    pos = at + last();
+    if (pos >= end) return false;
+    at = pos;
+    cost = cost_of(a, pr, ++tile);
+    if (cost == 0) {
+      tile = 0;
+      if (++h == a.g.hkv) h = 0, pr = problem_of(a, ++b);
+      while ((cost = cost_of(a, pr, 0)) == 0) pr = problem_of(a, ++b);  // (pos < total: a unit follows)
+    }
+    return true;
+  }
+};
+
 __device__ __forceinline__ void store_agent(float* p, float x, float y) {  // 8-byte device-scope store (p is 8-byte aligned)
   __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x),
                      __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -247,6 +330,21 @@ __device__ __forceinline__ void store_agent(float* p, float x, float y) {  // 8-
 __device__ __forceinline__ float2v load_agent(const float* p) {
   const unsigned long long u = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return float2v{__uint_as_float((unsigned)u), __uint_as_float((unsigned)(u >> 32))};
+}
+// Counts the workgroup in at a unit that begins in run first_run and reaches into `live`; whether it is the last of them.  (A run
+// is the first of one such unit at most, so its number names the unit's counter.)  The partials are device-scope stores, which no
+// cache holds back; each wave waits until its own are acknowledged, then one thread counts, and the workgroup that counts last
+// reads all partials with device-scope loads.  Nobody waits for anybody else.
+__device__ __forceinline__ bool arrives_last(const Args& a, int first_run, int live, int& arrived) {
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int* cnt = a.counters + first_run * kCounterInts;
+    arrived = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (arrived == live - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
+  }
+  __syncthreads();
+  return arrived == live - 1;
 }
 // factor of a part whose maximum is m in a sum under the maximum M
 __device__ __forceinline__ float part_factor(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
@@ -274,42 +372,19 @@ template <int D, int CODE, bool BF>
 __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   constexpr int kCh = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), kg = lane >> 4, n = lane & 15;
-  // the whole list's length, and the unit in which this run begins
-  const int run = blockIdx.x;
-  int total = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) total += wave_sum(b0 + lane < a.batch ? sequence_cost(a, b0 + lane) : 0);
-  const int per = max(a.per, (total + a.n_splits - 1) / a.n_splits);
-  if (run * per >= total) return;  // (also where no sequence has a query)
-  int pos = run * per, b = 0, at = 0;  // at: where sequence b begins
-  const int end = min(pos + per, total);
-  for (int b0 = 0, before = 0; b0 < a.batch; b0 += 64) {
-    const int cost = b0 + lane < a.batch ? sequence_cost(a, b0 + lane) : 0, upto = before + wave_prefix_sum(cost);
-    const unsigned long long found = __ballot(pos < upto);
-    if (found) {
-      const int k = __ffsll(found) - 1;
-      b = b0 + k, at = __builtin_amdgcn_readlane(upto - cost, k);
-      break;
-    }
-    before = __builtin_amdgcn_readlane(upto, 63);
-  }
+  Cursor<16> cur;
+  if (!cur.begin(a, blockIdx.x)) return;
   constexpr int kStride = D + 4;
   __shared__ __attribute__((aligned(16))) float sm_o[kWaves][16][kStride];
   __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
   __shared__ int arrived;
-  Problem pr = problem_of(a, b);
-  int tile = 0, h = 0;
-  for (int c; at + (c = unit_cost(a, pr, tile) * a.g.hkv) <= pos; ++tile) at += c;
-  {
-    const int c = unit_cost(a, pr, tile);
-    h = (pos - at) / c;
-    at += h * c;  // where the unit begins
-  }
-  while (true) {  // segments
-  const int cost = unit_cost(a, pr, tile), n_rows = pr.nq * a.g.ratio, r0 = tile * 16, r = r0 + n;
+  do {  // segments
+  const int b = cur.b, h = cur.h;
+  const Problem pr = cur.pr;
+  const int n_rows = pr.nq * a.g.ratio, r0 = cur.tile * 16, r = r0 + n;
   const int vis_min = visible(a, pr, r0 / a.g.ratio), blocks = (visible(a, pr, min(r0 + 15, n_rows - 1) / a.g.ratio) + kBlock - 1) / kBlock;
   const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : pr.len;
-  const int blk0 = pos - at, blk1 = min(min(blocks, cost), blk0 + end - pos);
-  const int first_run = at / per, live = (at + cost - 1) / per - first_run + 1;  // the runs that the unit reaches into
+  const int blk0 = cur.first(), blk1 = min(blocks, cur.last()), first_run = cur.first_run(), live = cur.runs();
   const int64_t line0 = ((int64_t)b * a.g.hkv + h) * a.rows + r0;
 
   auto fetch = [&](Fetched<D>& x, int blk) {  // (always loads: block 0 of the cache in the place of one that is not there)
@@ -452,23 +527,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       return;
     }
     if (row < rows_here) {
-      float* P = partial_of(run - first_run) + row * (D + 2);
+      float* P = partial_of(cur.run - first_run) + row * (D + 2);
 #pragma unroll
       for (int i = 0; i < kCh; i += 2) store_agent(P + c0 + i, acc[i], acc[i + 1]);
       if (c0 == 0) store_agent(P + D, M, L);
     }
   }
-  // The partials are device-scope stores (no cache holds them back); each wave waits until its own are acknowledged, then one
-  // thread counts the workgroup in, and the one that counts last reads all with device-scope loads.
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-  if (tid == 0) {
-    int* cnt = a.counters + first_run * kCounterInts;
-    arrived = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (arrived == live - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
-  }
-  __syncthreads();
-  if (arrived != live - 1) return;
+  if (!arrives_last(a, first_run, live, arrived)) return;
   // groups of 16 threads take (row, every G-th split); few rows leave more groups per row, which are joined through LDS
   int shift = 0;
   while ((1 << shift) < rows_here) ++shift;
@@ -526,20 +591,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   }
   write_row<D, BF, kCh>(a, b, h, r0 + row, c0, Mt, L, acc);
   }();
-  pos += min(cost - blk0, end - pos);
-  if (pos >= end) break;
-  // the next unit (one with rows: pos < total)
-  at = pos;
-  if (++h == a.g.hkv) {
-    h = 0, ++tile;
-    while (unit_cost(a, pr, tile) == 0) pr = problem_of(a, ++b), tile = 0;
-  }
   __syncthreads();  // the joining has left LDS
-  }
+  } while (cur.next(a));
 }
 
 // ---- many rows: tiles in LDS ------------------------------------------------------------------------------
-// One workgroup of four waves per 128 rows (and split), a wave holding 32 of them.  Each 64-token tile of keys and values is
+// Units of 128 rows, a wave holding 32 of them.  Each 64-token tile of keys and values is
 // converted once per workgroup and staged in LDS as fp16: keys token by token, values transposed, in the order in which the score
 // product leaves the weights in a lane, so that both products read their first operand as 16-byte rows and the weights never
 // leave their lane.  The next tile's codes are on their way to registers while a tile is worked on; two tiles in LDS, one barrier a tile.
@@ -563,21 +620,22 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
   constexpr int kCh = D / 16, kTok = 256 / D, kCellsOf4 = 4 / kTok, kKeyCells = D / 64;
   __shared__ ChunkTile<D> sm[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), hh = lane >> 5, n = lane & 31;
-  // (sequence, head, split) is the fastest index: workgroups that read the same keys fall on the same compute die where their
-  // number is a multiple of eight; the last tiles, which see most under a causal mask, come first
-  const int units = a.g.hkv * a.n_splits, tiles = (a.rows + 32 * kWaves - 1) / (32 * kWaves);
-  const int unit = blockIdx.x % units, tile = tiles - 1 - blockIdx.x / units, b = blockIdx.y;
-  const int h = unit % a.g.hkv, split = unit / a.g.hkv;
-  const Problem pr = problem_of(a, b);
-  const int n_rows = pr.nq * a.g.ratio, r0 = tile * 32 * kWaves;
-  if (r0 >= n_rows) return;
+  __shared__ int arrived;
+  // the workgroups of a compute die (every eighth) take runs that follow each other, so that they read the same keys
+  Cursor<32 * kWaves> cur;
+  const int dies = gridDim.x % 8 == 0 && !a.direct ? 8 : 1;
+  if (!cur.begin(a, blockIdx.x % dies * (gridDim.x / dies) + blockIdx.x / dies)) return;
+  do {  // segments
+  const int b = cur.b, h = cur.h;
+  const Problem pr = cur.pr;
+  const int n_rows = pr.nq * a.g.ratio, r0 = cur.tile * 32 * kWaves;
   const int rw = r0 + wave * 32, r = rw + n;
   const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : pr.len;
   // what the wave's and the workgroup's rows see at least and at most
   const int last = min(rw + 31, n_rows - 1);
   const int vis_min = rw < n_rows ? visible(a, pr, rw / a.g.ratio) : 0, vis_max = rw < n_rows ? visible(a, pr, last / a.g.ratio) : 0;
   const int vis_all = visible(a, pr, min(r0 + 32 * kWaves - 1, n_rows - 1) / a.g.ratio);
-  const int blk0 = split * a.per, blk1 = min(blk0 + a.per, (vis_all + kBlock - 1) / kBlock);
+  const int blk0 = cur.first(), blk1 = min((vis_all + kBlock - 1) / kBlock, cur.last()), first_run = cur.first_run(), live = cur.runs();
 
   half8v q[D / 16];
   const float factor = load_query_rows<D, BF>(a, b, h, r, pr.nq, q);
@@ -742,71 +800,68 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     }
     if (blk + 1 < blk1 && next_there) stage(sm[buf ^ 1]);
   }
-  if (r >= n_rows) return;
   l += __shfl_xor(l, 32, 64);
   // o[i][e]: row 32 i + 8 (e / 4) + 4 hh + e % 4 of the transposed values; the channels of cell c are its rows 16 x + c
-  const int64_t line = ((int64_t)b * a.g.hkv + h) * a.rows + r;
-  const float M = m - kLift;
+  float M = l == 0.f ? -INFINITY : m - kLift, unit_of_o = sref;
+  [&] {
+  if (live > 1) {
+    // the sums as they lie in the threads, two to a store; joined in the order of the runs
+    constexpr int kPairs = D / 4, kThreads = kWaves * 64;
+    auto partial_of = [&](int k) { return a.partial + (((int64_t)(first_run + k) * 2 + (k == 0)) * (kPairs + 1) * kThreads + tid) * 2; };
+    float* P = partial_of(cur.run - first_run);
+    if (r < n_rows) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) store_agent(P + (8 * i + e / 2) * kThreads * 2, o[i][e] * sref, o[i][e + 1] * sref);
+      store_agent(P + kPairs * kThreads * 2, M, l);
+    }
+    if (!arrives_last(a, first_run, live, arrived)) return;
+    M = -INFINITY, l = 0.f, unit_of_o = 1.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    if (r < n_rows)
+      for (int k = 0; k < live; ++k) {
+        const float* ps = partial_of(k);
+        const float2v ml = load_agent(ps + kPairs * kThreads * 2);
+        float2v x[kPairs];
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) x[i] = load_agent(ps + i * kThreads * 2);
+        const float m2 = fmaxf(M, ml[0]), turn = part_factor(M, m2), f = part_factor(ml[0], m2);
+        M = m2;
+        l = fmaf(f, ml[1], l * turn);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[i][e] = fmaf(f, x[8 * i + e / 2][e & 1], o[i][e] * turn);
+      }
+  }
+  if (r >= n_rows) return;
   const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;
-  const float inv = a.n_splits > 1 ? sref : l > 0.f ? sref / l : (l == 0.f ? 0.f : l);
+  const float inv = l > 0.f ? unit_of_o / l : (l == 0.f ? 0.f : l);
 #pragma unroll
   for (int c4 = 0; c4 < 2; ++c4)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int cell = 8 * c4 + 4 * hh + e;
-      float x[kCh];
+      alignas(16) uint16_t u[kCh];
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) x[i] = o[i / 2][8 * (i & 1) + 4 * c4 + e] * inv;
-      if (a.n_splits > 1) {
-        float* P = a.partial + (line * a.n_splits + split) * (D + 2) + kCh * cell;
-#pragma unroll
-        for (int i = 0; i < kCh; i += 2) *reinterpret_cast<float2v*>(P + i) = float2v{x[i], x[i + 1]};
-      } else {
-        alignas(16) uint16_t u[kCh];
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) u[i] = from_float<BF>(x[i]);
-        if constexpr (kCh == 8)
-          *reinterpret_cast<uint4v*>(a.out + place * D + kCh * cell) = *reinterpret_cast<const uint4v*>(u);
-        else
-          *reinterpret_cast<uint2v*>(a.out + place * D + kCh * cell) = *reinterpret_cast<const uint2v*>(u);
-      }
+      for (int i = 0; i < kCh; ++i) u[i] = from_float<BF>(o[i / 2][8 * (i & 1) + 4 * c4 + e] * inv);
+      uint16_t* to = a.out + place * D + kCh * (8 * c4 + 4 * hh + e);
+      if constexpr (kCh == 8)
+        *reinterpret_cast<uint4v*>(to) = *reinterpret_cast<const uint4v*>(u);
+      else
+        *reinterpret_cast<uint2v*>(to) = *reinterpret_cast<const uint2v*>(u);
     }
   if (hh == 0) {
-    if (a.n_splits > 1) {
-      float* P = a.partial + (line * a.n_splits + split) * (D + 2);
-      P[D] = l == 0.f ? -INFINITY : M, P[D + 1] = l;
-    } else {
-      const float z = l == 0.f ? -INFINITY : M + __log2f(l);
-      if (a.lse) a.lse[place] = z * kLn2;
-      a.lse2[line] = z;
-    }
-  }
-}
-
-// the splits of a chunk's rows are joined: one workgroup of D threads per row
-template <int D, bool BF>
-__global__ __launch_bounds__(D) void merge_kernel(Args a) {
-  const int r = blockIdx.x / a.g.hkv, h = blockIdx.x % a.g.hkv, b = blockIdx.y, c = threadIdx.x;
-  const Problem pr = problem_of(a, b);
-  if (r >= pr.nq * a.g.ratio) return;
-  const int64_t line = ((int64_t)b * a.g.hkv + h) * a.rows + r;
-  const float* P = a.partial + line * a.n_splits * (D + 2);
-  float M = -INFINITY, L = 0.f, acc = 0.f;
-  for (int s = 0; s < a.n_splits; ++s) M = fmaxf(M, P[s * (D + 2) + D]);
-  for (int s = 0; s < a.n_splits; ++s) {
-    const float ms = P[s * (D + 2) + D];
-    const float e = part_factor(ms, M);
-    L = fmaf(e, P[s * (D + 2) + D + 1], L);
-    acc = fmaf(e, P[s * (D + 2) + c], acc);
-  }
-  const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;
-  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
-  a.out[place * D + c] = from_float<BF>(acc * inv);
-  if (c == 0) {
-    const float z = L == 0.f ? -INFINITY : M + __log2f(L);
+    const float z = l == 0.f ? -INFINITY : M + __log2f(l);
     if (a.lse) a.lse[place] = z * kLn2;
-    a.lse2[line] = z;
+    a.lse2[((int64_t)b * a.g.hkv + h) * a.rows + r] = z;
   }
+  }();
+  __syncthreads();  // everybody has left the tiles in LDS
+  } while (cur.next(a));
 }
 
 // ---- the weights that each cached token receives ----------------------------------------------------------
@@ -891,9 +946,9 @@ static size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 // How a call is cut, and where its workspace's parts lie
 struct Plan {
-  bool chunk;
+  bool chunk, direct;
   int64_t tiles;  // of rows
-  int splits, per;
+  int runs, per;
   bool scores;
   size_t lse2_at, partial_at, scores_at, bytes;
   int64_t score_stride;
@@ -902,29 +957,24 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   Plan p;
   const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads), lines = rows * s.n_kv_heads * batch;
   p.chunk = use_chunk(rows);
-  const int per_tile = p.chunk ? 32 * kWaves : 16;
-  p.tiles = (rows + per_tile - 1) / per_tile;
+  const int tile_rows = p.chunk ? 32 * kWaves : 16;
+  p.tiles = (rows + tile_rows - 1) / tile_rows;
   const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
-  const int64_t groups = p.tiles * s.n_kv_heads * batch;
-  size_t partials = 0;
-  if (p.chunk) {
-    const int64_t splits = requested > 0 ? requested : std::min<int64_t>((blocks + 7) / 8, 512 / groups);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, blocks));
-    p.per = (blocks + p.splits - 1) / p.splits;
-    if (p.splits > 1) partials = (size_t)lines * p.splits;
-  } else {
-    // runs: two workgroups to each of the 256 compute units, or one per unit where there are more; four blocks at least (a wave
-    // each), as a run's start and joining take as long as some blocks
-    p.per = requested > 0 ? 1 : kWaves;
-    const int64_t runs = requested > 0 ? requested * groups : std::max<int64_t>(512, groups);
-    p.splits = (int)std::min<int64_t>(std::min<int64_t>(runs, kMaxCounters), (groups * blocks + p.per - 1) / p.per);
-    partials = (size_t)p.splits * 2 * 16;
-  }
+  const int64_t units = p.tiles * s.n_kv_heads * batch;
+  // runs: two workgroups to each of the 256 compute units (few rows: or one per unit where there are more); four blocks at least (few
+  // rows: a wave each), as a run's start and joining take as long as some blocks
+  const int64_t most = p.chunk ? 512 : kMaxCounters;
+  p.direct = requested <= 0 && (p.chunk ? units >= 1024 : units > most);
+  p.per = requested > 0 ? 1 : 4;
+  const int64_t runs = requested > 0 ? requested * units : p.chunk ? 512 : std::max<int64_t>(512, units);
+  p.runs = p.direct ? (int)std::min<int64_t>(units, 0x7fffffff)
+                    : (int)std::min<int64_t>(std::min<int64_t>(runs, most), (units * blocks + p.per - 1) / p.per);
+  const size_t partials = p.direct ? 0 : (size_t)p.runs * 2 * (p.chunk ? (s.head_dim / 2 + 2) * kWaves * 64 : 16 * (s.head_dim + 2));
   p.scores = weights && rows <= 16;
   p.score_stride = (int64_t)blocks * kBlock;
   p.lse2_at = (size_t)kMaxCounters * kCounterInts * sizeof(int);
   p.partial_at = p.lse2_at + up16(lines * sizeof(float));
-  p.scores_at = p.partial_at + up16(partials * (s.head_dim + 2) * sizeof(float));
+  p.scores_at = p.partial_at + up16(partials * sizeof(float));
   p.bytes = p.scores_at + (p.scores ? (size_t)lines * p.score_stride * sizeof(float) : 0);
   return p;
 }
@@ -944,7 +994,7 @@ int attention_launch(const AttentionCall& c) {
   a.kc = make_view(c.kc), a.vc = make_view(c.vc);
   a.seq_lens = c.seq_lens, a.max_seq_len = c.max_seq_len;
   a.scale_log2 = c.scale * kLog2e, a.causal = c.causal;
-  a.batch = c.batch, a.n_splits = plan.splits, a.per = plan.per;
+  a.batch = c.batch, a.n_runs = plan.runs, a.per = plan.per, a.direct = plan.direct;
   a.out = static_cast<uint16_t*>(c.out), a.lse = c.lse;
   a.counters = reinterpret_cast<int*>(ws);
   a.row_tiles = (int)plan.tiles;
@@ -956,20 +1006,16 @@ int attention_launch(const AttentionCall& c) {
   return with_types(s, [&](auto d, auto code, auto bf) -> int {
     constexpr int D = decltype(d)::value, CODE = decltype(code)::value;
     constexpr bool BF = decltype(bf)::value;
-    const int64_t groups = plan.tiles * a.g.hkv * plan.splits, listed = plan.tiles * a.g.hkv * c.batch * (a.score_stride / kBlock);
-    if (plan.chunk ? groups > 0x7fffffff || (int64_t)a.rows * a.g.hkv > 0x7fffffff : listed > 0x3fffffff) {
+    const int64_t units = plan.tiles * a.g.hkv * c.batch;
+    if (plan.direct ? units > 0x7fffffff : units * (a.score_stride / kBlock) > 0x3fffffff) {
       set_error("q8_attention: batch * n_q * n_q_heads * max_seq_len is too large for one launch");
       return NSN_ERR_UNSUPPORTED;
     }
     if (plan.chunk)
-      chunk_kernel<D, CODE, BF><<<dim3((unsigned)groups, c.batch), kWaves * 64, 0, c.stream>>>(a);
+      chunk_kernel<D, CODE, BF><<<plan.runs, kWaves * 64, 0, c.stream>>>(a);
     else
-      rows_kernel<D, CODE, BF><<<plan.splits, kWaves * 64, 0, c.stream>>>(a);
+      rows_kernel<D, CODE, BF><<<plan.runs, kWaves * 64, 0, c.stream>>>(a);
     if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
-    if (plan.chunk && plan.splits > 1) {
-      merge_kernel<D, BF><<<dim3(a.rows * a.g.hkv, c.batch), D, 0, c.stream>>>(a);
-      if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
-    }
     if (a.weights_out && c.max_seq_len > 0) {
       if (plan.scores)
         weights_of_scores_kernel<<<dim3((c.max_seq_len + 4 * kScoreThreads - 1) / (4 * kScoreThreads), a.g.hkv, c.batch), kScoreThreads, 0, c.stream>>>(a);

@@ -42,6 +42,7 @@ struct Args {
   int row_tiles;
   float* scores;   // [batch][hkv][rows][score_stride] in powers of two, -infinity where nothing is seen (workspace), or NULL
   int64_t score_stride;
+  int weight_parts;  // of the rows, in the pass that adds weights up
   const float* weights_in;
   float* weights_out;
 };
@@ -865,53 +866,160 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
 }
 
 // ---- the weights that each cached token receives ----------------------------------------------------------
-// One workgroup per 64-token block and kv head: the block's keys stay in registers, its waves go through the rows 16 at a
-// time, add 2^(s - lse) up per token, and are joined in a fixed order.
+// One workgroup per 256 tokens of a kv head and part of the rows: each wave holds 64 tokens' keys as operands in registers (in the
+// queries' own type, which codes fit without loss), the rows come by in LDS tiles of 32 that all four waves read, and a wave adds
+// 2^(s - lse) up per token.  Parts are joined in their order by the last workgroup to arrive.  Bound by the exponentials: one
+// per row and token, a quarter of the vector rate, with the products beside them.
+constexpr int kWeightTokens = 64 * kWaves, kWeightRows = 32;
+
+template <int CODE, bool BF>
+__device__ __forceinline__ uint4v to_operand8(unsigned w0, unsigned w1) {
+  if constexpr (!BF) {
+    half2v a, b, c, d;
+    to_half4<CODE>(w0, a, b);
+    to_half4<CODE>(w1, c, d);
+    return __builtin_bit_cast(uint4v, (half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}));
+  } else {  // (codes have 8 significant bits at most: the upper half of the fp32 number is the bf16 one)
+    float f[8];
+    to_float4<CODE>(w0, f);
+    to_float4<CODE>(w1, f + 4);
+    uint4v u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_perm(__float_as_uint(f[2 * i + 1]), __float_as_uint(f[2 * i]), 0x07060302u);
+    return u;
+  }
+}
+typedef __bf16 bfloat8v __attribute__((ext_vector_type(8)));
+template <bool BF>
+__device__ __forceinline__ float16v product32(uint4v x, uint4v y, float16v c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bfloat8v, x), __builtin_bit_cast(bfloat8v, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, x), __builtin_bit_cast(half8v, y), c, 0, 0, 0);
+}
+
 template <int D, int CODE, bool BF>
-__global__ __launch_bounds__(kWaves * 64) void weights_kernel(Args a) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), kg = lane >> 4, n = lane & 15;
-  const int blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+__global__ __launch_bounds__(kWaves * 64, 2) void weights_kernel(Args a) {
+  constexpr int kPieces = kWeightRows * D / 8 / (kWaves * 64);  // 16-byte pieces of a tile of rows that a thread brings
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), hh = lane >> 5, n = lane & 31;
+  const int part = blockIdx.x % a.weight_parts, group = blockIdx.x / a.weight_parts, h = blockIdx.y, b = blockIdx.z;
   const Problem pr = problem_of(a, b);
-  const int t0 = blk * kBlock, n_rows = pr.nq * a.g.ratio;
-  if (t0 >= pr.len) return;
-  const int64_t pk = block_place(a.g, a.kc.block_table, b, h, blk), pv = block_place(a.g, a.vc.block_table, b, h, blk);
-  float4v sum[4];
+  const int g0 = group * kWeightTokens, t0 = g0 + wave * kBlock, n_rows = pr.nq * a.g.ratio;
+  if (g0 >= pr.len) return;
+  __shared__ __attribute__((aligned(16))) uint16_t sm_q[2][kWeightRows][D + 8];
+  __shared__ float sm_z[2][kWeightRows];
+  __shared__ int arrived;
+  // the rows that see the first token of the group, cut into the parts
+  const int first = a.causal ? min(max(g0 - pr.vis0 + 1, 0), pr.nq) * a.g.ratio / kWeightRows : 0;
+  const int tiles = (n_rows + kWeightRows - 1) / kWeightRows - first, per = (tiles + a.weight_parts - 1) / a.weight_parts;
+  const int tile0 = first + min(part * per, tiles), tile1 = first + min((part + 1) * per, tiles);
+
+  uint4v k[2][D / 16];
+  float f = 0.f;
+  float16v sum[2];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) sum[j] = float4v{0.f, 0.f, 0.f, 0.f};
-  if (pk >= 0 && pv >= 0) {
-    KeyCodes<D> kw;
-    kw.load(a.kc.codes + pk * (int64_t)(kBlock * D));
-    const float sk = a.kc.scales[pk];
-    for (int r0 = wave * 16; r0 < n_rows; r0 += kWaves * 16) {
-      if (visible(a, pr, min(r0 + 15, n_rows - 1) / a.g.ratio) <= t0) continue;
-      const int r = r0 + n;
-      half8v q[D / 32];
-      const float f = load_queries<D, BF>(a, b, h, r, pr.nq, q) * sk;
-      const float z = r < n_rows ? a.lse2[((int64_t)b * a.g.hkv + h) * a.rows + r] : INFINITY;
-      const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : 0;
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float4v s = {0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < 16; ++e) sum[j][e] = 0.f;
+  bool there = t0 < pr.len;
+  if (there) {
+    const int64_t pk = block_place(a.g, a.kc.block_table, b, h, t0 / kBlock), pv = block_place(a.g, a.vc.block_table, b, h, t0 / kBlock);
+    there = pk >= 0 && pv >= 0;
+    if (there) {
+      const uint8_t* p = a.kc.codes + pk * (int64_t)(kBlock * D) + 8 * hh;
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) s = __builtin_amdgcn_mfma_f32_16x16x32_f16(kw.template operand<CODE>(j, ks), q[ks], s, 0, 0, 0);
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[j][e] += t0 + 16 * j + 4 * kg + e < vis ? fast_exp2(fmaf(s[e], f, -z)) : 0.f;
-      }
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint2v w = *reinterpret_cast<const uint2v*>(p + (32 * j + n) * D + 16 * ks);
+          k[j][ks] = to_operand8<CODE, BF>(w[0], w[1]);
+        }
+      f = a.scale_log2 * a.kc.scales[pk];
     }
   }
-  // over the 16 rows of a tile, then over the waves
-  __shared__ float sm[kWaves][kBlock];
+  uint4v piece[kPieces];
+  float z = 0.f;
+  auto fetch = [&](int tile) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+    for (int i = 0; i < kPieces; ++i) {
+      const int x = tid + i * kWaves * 64, r = tile * kWeightRows + x / (D / 8);
+      piece[i] = uint4v{0, 0, 0, 0};
+      if (r < n_rows)
+        piece[i] = *reinterpret_cast<const uint4v*>(a.q.data + b * a.q.sb + (h * a.g.ratio + r % a.g.ratio) * a.q.sh + r / a.g.ratio * a.q.st + x % (D / 8) * 8);
+    }
+    if (tid < kWeightRows) {
+      const int r = tile * kWeightRows + tid;
+      z = r < n_rows ? a.lse2[((int64_t)b * a.g.hkv + h) * a.rows + r] : INFINITY;
+      if (z == -INFINITY) z = INFINITY;  // (a row that sees nothing gives nothing)
+    }
+  };
+  auto stage = [&](int buf) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = xor_sum_w<16>(sum[j][e]);
-      if (n == 0) sm[wave][16 * j + 4 * kg + e] = x;
+    for (int i = 0; i < kPieces; ++i) {
+      const int x = tid + i * kWaves * 64;
+      *reinterpret_cast<uint4v*>(&sm_q[buf][x / (D / 8)][x % (D / 8) * 8]) = piece[i];
+    }
+    if (tid < kWeightRows) sm_z[buf][tid] = z;
+  };
+  if (tile0 < tile1) {
+    fetch(tile0);
+    stage(0);
+  }
+  for (int tile = tile0, buf = 0; tile < tile1; ++tile, buf ^= 1) {
+    __syncthreads();
+    if (tile + 1 < tile1) fetch(tile + 1);
+    const int r0 = tile * kWeightRows, r = r0 + n;
+    if (there && visible(a, pr, min(r0 + kWeightRows - 1, n_rows - 1) / a.g.ratio) > t0) {
+      float16v s[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const uint4v q = *reinterpret_cast<const uint4v*>(&sm_q[buf][n][16 * ks + 8 * hh]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) s[j] = product32<BF>(k[j][ks], q, s[j]);
+      }
+      const float zr = sm_z[buf][n];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[j][e] = fast_exp2(fmaf(s[j][e], f, -zr));
+      if (visible(a, pr, r0 / a.g.ratio) < t0 + kBlock) {
+        const int vis = r < n_rows ? visible(a, pr, r / a.g.ratio) : 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) s[j][e] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) sum[j] += s[j];
+    }
+    if (tile + 1 < tile1) stage(buf ^ 1);
+  }
+  // over the 32 rows of a tile: one value per token, token 32 j + 8 (e / 4) + 4 hh + e % 4 of the wave in lane 0 of its half
+  __shared__ float sm[kWeightTokens];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float x = xor_sum_w<32>(sum[j][e]);
+      if (n == 0) sm[wave * kBlock + 32 * j + 8 * (e / 4) + 4 * hh + e % 4] = x;
     }
   __syncthreads();
-  if (tid < kBlock && t0 + tid < pr.len) {
-    const int64_t at = ((int64_t)b * a.g.hkv + h) * a.g.max_len + t0 + tid;
-    const float x = (sm[0][tid] + sm[1][tid]) + (sm[2][tid] + sm[3][tid]);
+  float x = sm[tid];
+  if (a.weight_parts > 1) {
+    const int64_t place = ((int64_t)(b * gridDim.y + h) * (gridDim.x / a.weight_parts) + group) * a.weight_parts;
+    float* P = a.partial + place * kWeightTokens + tid;
+    __hip_atomic_store(P + part * kWeightTokens, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!arrives_last(a, (int)(place / a.weight_parts), a.weight_parts, arrived)) return;
+    x = 0.f;
+    for (int i = 0; i < a.weight_parts; ++i) x += __hip_atomic_load(P + i * kWeightTokens, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (g0 + tid < pr.len) {
+    const int64_t at = ((int64_t)b * a.g.hkv + h) * a.g.max_len + g0 + tid;
     a.weights_out[at] = a.weights_in ? a.weights_in[at] + x : x;
   }
 }
@@ -950,10 +1058,13 @@ struct Plan {
   int64_t tiles;  // of rows
   int runs, per;
   bool scores;
+  int64_t weight_groups;  // of 256 tokens
+  int weight_parts;
   size_t lse2_at, partial_at, scores_at, bytes;
   int64_t score_stride;
 };
-static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int requested, bool weights) {
+// ragged: sequences may have fewer queries than n_q
+static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int requested, bool weights, bool ragged) {
   Plan p;
   const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads), lines = rows * s.n_kv_heads * batch;
   p.chunk = use_chunk(rows);
@@ -964,13 +1075,20 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   // runs: two workgroups to each of the 256 compute units (few rows: or one per unit where there are more); four blocks at least (few
   // rows: a wave each), as a run's start and joining take as long as some blocks
   const int64_t most = p.chunk ? 512 : kMaxCounters;
-  p.direct = requested <= 0 && (p.chunk ? units >= 1024 : units > most);
+  // chunks of many units go one to a workgroup, as joining a cut tile's 128 rows costs about ten of its blocks: with 512 units of 128 to
+  // 160 blocks 355 us so and 372 us in equal runs; with ragged chunks of up to 512 units of very different lengths 114 us and 62 us
+  p.direct = requested <= 0 && (p.chunk ? units >= (ragged ? 1024 : 512) : units > most);
   p.per = requested > 0 ? 1 : 4;
   const int64_t runs = requested > 0 ? requested * units : p.chunk ? 512 : std::max<int64_t>(512, units);
   p.runs = p.direct ? (int)std::min<int64_t>(units, 0x7fffffff)
                     : (int)std::min<int64_t>(std::min<int64_t>(runs, most), (units * blocks + p.per - 1) / p.per);
-  const size_t partials = p.direct ? 0 : (size_t)p.runs * 2 * (p.chunk ? (s.head_dim / 2 + 2) * kWaves * 64 : 16 * (s.head_dim + 2));
+  // the pass that adds weights up: up to eight workgroups to a compute unit, as sequences may be shorter than max_seq_len and causal
+  // parts unequal, each with four tiles of rows at least; its partial sums come after the attention's and take their place
+  p.weight_groups = (blocks + kWaves - 1) / kWaves * (int64_t)s.n_kv_heads * batch;
+  p.weight_parts = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCounters / p.weight_groups, rows / (4 * kWeightRows)));
+  size_t partials = p.direct ? 0 : (size_t)p.runs * 2 * (p.chunk ? (s.head_dim / 2 + 2) * kWaves * 64 : 16 * (s.head_dim + 2));
   p.scores = weights && rows <= 16;
+  if (weights && p.weight_parts > 1) partials = std::max(partials, (size_t)p.weight_groups * p.weight_parts * kWeightTokens);
   p.score_stride = (int64_t)blocks * kBlock;
   p.lse2_at = (size_t)kMaxCounters * kCounterInts * sizeof(int);
   p.partial_at = p.lse2_at + up16(lines * sizeof(float));
@@ -980,12 +1098,12 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
 }
 
 size_t attention_workspace_bytes(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int n_splits, bool weights) {
-  return plan_of(s, batch, n_q, max_seq_len, n_splits, weights).bytes;
+  return std::max(plan_of(s, batch, n_q, max_seq_len, n_splits, weights, false).bytes, plan_of(s, batch, n_q, max_seq_len, n_splits, weights, true).bytes);
 }
 
 int attention_launch(const AttentionCall& c) {
   const nsn_q8_shape& s = c.shape;
-  const Plan plan = plan_of(s, c.batch, c.n_q, c.max_seq_len, c.n_splits, c.weights_out != nullptr);
+  const Plan plan = plan_of(s, c.batch, c.n_q, c.max_seq_len, c.n_splits, c.weights_out != nullptr, c.q_lens != nullptr);
   unsigned char* ws = static_cast<unsigned char*>(c.workspace);
   Args a;
   a.g = make_geometry(s);
@@ -1002,6 +1120,7 @@ int attention_launch(const AttentionCall& c) {
   a.partial = reinterpret_cast<float*>(ws + plan.partial_at);
   a.scores = plan.scores ? reinterpret_cast<float*>(ws + plan.scores_at) : nullptr;
   a.score_stride = plan.score_stride;
+  a.weight_parts = plan.weight_parts;
   a.weights_in = c.weights_in, a.weights_out = c.weights_out;
   return with_types(s, [&](auto d, auto code, auto bf) -> int {
     constexpr int D = decltype(d)::value, CODE = decltype(code)::value;
@@ -1020,7 +1139,7 @@ int attention_launch(const AttentionCall& c) {
       if (plan.scores)
         weights_of_scores_kernel<<<dim3((c.max_seq_len + 4 * kScoreThreads - 1) / (4 * kScoreThreads), a.g.hkv, c.batch), kScoreThreads, 0, c.stream>>>(a);
       else
-        weights_kernel<D, CODE, BF><<<dim3((c.max_seq_len + kBlock - 1) / kBlock, a.g.hkv, c.batch), kWaves * 64, 0, c.stream>>>(a);
+        weights_kernel<D, CODE, BF><<<dim3((c.max_seq_len + kWeightTokens - 1) / kWeightTokens * plan.weight_parts, a.g.hkv, c.batch), kWaves * 64, 0, c.stream>>>(a);
       if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
     }
     return NSN_OK;

@@ -131,6 +131,16 @@ __device__ __forceinline__ uint16_t from_float(float f) {  // to nearest even
     return __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
+__device__ __forceinline__ int wave_scan(int v) {  // inclusive prefix sum over the 64 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row 0's and 2's last lane to the rows behind them
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the lower half's last lane to the upper half
+  return v;
+}
+
 inline Geometry make_geometry(const nsn_q8_shape& s) {
   Geometry g;
   g.hq = s.n_q_heads, g.hkv = s.n_kv_heads, g.ratio = s.n_q_heads / s.n_kv_heads;

@@ -216,16 +216,6 @@ struct Fetched {
 // head, tile).  It is cut into equal runs, one workgroup each, whatever the sequences' lengths: all workgroups end at about
 // the same time, where a grid over units and splits leaves a last round that few take part in.  A run is a few segments, each of one
 // unit.  A unit that reaches into other runs leaves partial sums, which the last workgroup to arrive joins.
-__device__ __forceinline__ int wave_scan(int v) {  // inclusive prefix sum over the 64 lanes
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row 0's and 2's last lane to the rows behind them
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the lower half's last lane to the upper half
-  return v;
-}
-
 template <int TILE>
 struct Cursor {
   int b, h, tile, cost;  // the unit, and its blocks in the list

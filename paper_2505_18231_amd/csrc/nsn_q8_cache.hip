@@ -129,10 +129,13 @@ int append_launch(const nsn_q8_shape& s, const nsn_rows& k, const nsn_rows& v, i
 }
 
 // ---- eviction: which tokens stay ------------------------------------------------------------------------
-// One workgroup per (sequence, head).  The weights are ordered as unsigned keys (NaN the least); the need-th largest key of
-// the middle tokens is found eight bits at a time with a histogram per pass, then one pass over the tokens in order writes
-// those above it and the first of those that equal it.  Integer sums only: the same tokens for any order of the threads.
-constexpr int kSelThreads = 1024;
+// One workgroup per (sequence, head).  The weights, ordered as unsigned keys (NaN the least), stay in registers where a
+// sequence fits (16 to a thread; a longer one is read again for every pass).  The need-th largest key of the middle tokens is
+// found by digits of 11, 11 and 10 bits, with a histogram of each in LDS; then the tokens above it and the first of those that
+// equal it are counted off in order.  Integer sums only: the same tokens for any order of the threads.  Bound by the
+// histograms' additions to one address: the first lane's digit, often that of many lanes (weights of zero), is added once for all of
+// them, and a first digit of 11 bits spreads the others over four bins per power of two.
+constexpr int kBins = 2048;
 
 __device__ __forceinline__ unsigned weight_key(float w) {
   if (w != w) return 0u;
@@ -140,9 +143,26 @@ __device__ __forceinline__ unsigned weight_key(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kSelThreads) void select_kernel(int hkv, int max_len, const float* weights, const int32_t* seq_lens,
-                                                             int max_seq_len, int keep, int first, int recent, int32_t* kept,
-                                                             int32_t* new_lens, float* weights_out) {
+// inclusive prefix sums over the workgroup of two values per thread, and their totals; sums: T / 64 pairs of LDS
+template <int T>
+__device__ __forceinline__ void scan_pair(int& x, int& y, int& all_x, int& all_y, int (&sums)[2][T / 64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  x = wave_scan(x), y = wave_scan(y);
+  if (lane == 63) sums[0][wave] = x, sums[1][wave] = y;
+  __syncthreads();
+  all_x = all_y = 0;
+#pragma unroll
+  for (int i = 0; i < T / 64; ++i) {
+    const int sx = sums[0][i], sy = sums[1][i];
+    if (i < wave) x += sx, y += sy;
+    all_x += sx, all_y += sy;
+  }
+}
+
+template <int T, int K, bool RESIDENT>
+__global__ __launch_bounds__(T) void select_kernel(int hkv, int max_len, const float* weights, const int32_t* seq_lens, int max_seq_len,
+                                                   int keep, int first, int recent, int32_t* kept, int32_t* new_lens,
+                                                   float* weights_out) {
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int len = min(max(seq_lens[b], 0), max_seq_len);
   const int n_keep = min(len, keep);
@@ -152,170 +172,226 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(int hkv, int max_le
   float* wo = weights_out ? weights_out + unit * max_len : nullptr;
   if (h == 0 && tid == 0) new_lens[b] = n_keep;
 
-  __shared__ unsigned hist[256];
+  __shared__ int hist[kBins];
   __shared__ int found[2];
-  __shared__ int wsum[2][kSelThreads / 64];
+  __shared__ int sums[2][T / 64];
+  __shared__ int count[2][K * T / 64];
+  float v[K];  // token base + i * T + tid
+  auto load = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const int t = base + i * T + tid;
+      v[i] = t < len ? w[t] : 0.f;
+    }
+  };
+  if (RESIDENT) load(0);
+
   const int mid0 = first, mid1 = len - recent;  // the tokens to choose from, where len > keep
   unsigned prefix = 0, mask = 0;
   int need = keep - first - recent;
   const bool choose = len > keep && need > 0;
   if (choose) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+#pragma unroll
+    for (int digit = 0; digit < 3; ++digit) {
+      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
+      for (int i = tid; i < kBins; i += T) hist[i] = 0;
       __syncthreads();
-      for (int t = mid0 + tid; t < mid1; t += kSelThreads) {
-        const unsigned k = weight_key(w[t]);
-        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+      for (int base = 0; base < len; base += T * K) {
+        if (!RESIDENT) load(base);
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+          const int t = base + i * T + tid;
+          const unsigned k = weight_key(v[i]);
+          const bool in = t >= mid0 && t < mid1 && (k & mask) == prefix;
+          const unsigned long long lanes = __ballot(in);
+          if (lanes == 0) continue;
+          const int d = (int)(k >> shift) & ((1 << bits) - 1), lead = __ffsll(lanes) - 1, dl = __builtin_amdgcn_readlane(d, lead);
+          const unsigned long long same = __ballot(in && d == dl);
+          if (lane == lead)
+            atomicAdd(&hist[dl], (int)__popcll(same));
+          else if (in && d != dl)
+            atomicAdd(&hist[d], 1);
+        }
       }
       __syncthreads();
-      if (wave == 0) {  // lane l owns bins 4 l .. 4 l + 3; counts of the bins above
-        unsigned c[4], own_sum = 0;
+      constexpr int kOwn = kBins / T;  // bins of a thread
+      int c[kOwn], x = 0, y = 0, all = 0, none;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = hist[4 * lane + i], own_sum += c[i];
-        unsigned above = own_sum;
-        for (int m = 1; m < 64; m <<= 1) {
-          const unsigned o = __shfl_down(above, m, 64);
-          if (lane + m < 64) above += o;
-        }
-        above -= own_sum;
+      for (int i = 0; i < kOwn; ++i) c[i] = hist[tid * kOwn + i], x += c[i];
+      scan_pair<T>(x, y, all, none, sums);
+      int above = all - x;  // in the bins of the threads behind
 #pragma unroll
-        for (int i = 3; i >= 0; --i) {
-          if (above < (unsigned)need && above + c[i] >= (unsigned)need) found[0] = 4 * lane + i, found[1] = need - (int)above;
-          above += c[i];
-        }
+      for (int i = kOwn - 1; i >= 0; --i) {
+        if (above < need && above + c[i] >= need) found[0] = tid * kOwn + i, found[1] = need - above;
+        above += c[i];
       }
       __syncthreads();
       prefix |= (unsigned)found[0] << shift;
-      mask |= 255u << shift;
+      mask |= ((1u << bits) - 1) << shift;
       need = found[1];
     }
   }
-  // in order: need = how many of the tokens whose key equals `prefix` stay (the first ones)
-  int base = 0, base_eq = 0;
-  for (int t0 = 0; t0 < len; t0 += kSelThreads) {
-    const int t = t0 + tid;
-    bool sure = false, eq = false;
-    float wt = 0.f;
-    if (t < len) {
-      wt = w[t];
-      if (len <= keep || t < first || t >= mid1) {
-        sure = true;
-      } else if (choose) {
-        const unsigned k = weight_key(wt);
-        sure = k > prefix, eq = k == prefix;
+  // In order: tokens that stay whatever the others are, and the first `need` of those whose key equals `prefix`.
+  int base_sure = 0, base_eq = 0;
+  for (int base = 0; base < len; base += T * K) {
+    if (!RESIDENT) load(base);
+    unsigned long long sure[K], eq[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const int t = base + i * T + tid;
+      bool s = false, e = false;
+      if (t < len) {
+        if (len <= keep || t < first || t >= mid1) {
+          s = true;
+        } else if (choose) {
+          const unsigned k = weight_key(v[i]);
+          s = k > prefix, e = k == prefix;
+        }
+      }
+      sure[i] = __ballot(s), eq[i] = __ballot(e);
+      if (lane == 0) count[0][i * (T / 64) + wave] = __popcll(sure[i]), count[1][i * (T / 64) + wave] = __popcll(eq[i]);
+    }
+    __syncthreads();
+    static_assert(K * T / 64 <= T, "one count to a thread");
+    const int own_x = tid < K * T / 64 ? count[0][tid] : 0, own_y = tid < K * T / 64 ? count[1][tid] : 0;
+    int x = own_x, y = own_y, all_x, all_y;
+    scan_pair<T>(x, y, all_x, all_y, sums);
+    if (tid < K * T / 64) count[0][tid] = x - own_x, count[1][tid] = y - own_y;
+    __syncthreads();
+    const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const int before_eq = base_eq + count[1][i * (T / 64) + wave] + (int)__popcll(eq[i] & below);
+      const int at = base_sure + count[0][i * (T / 64) + wave] + (int)__popcll(sure[i] & below) + min(before_eq, need);
+      if ((sure[i] >> lane & 1) || ((eq[i] >> lane & 1) && before_eq < need)) {
+        kp[at] = base + i * T + tid;
+        if (wo) wo[at] = v[i];
       }
     }
-    const unsigned long long m_eq = __ballot(eq), below = (1ull << lane) - 1;
-    if (lane == 0) wsum[0][wave] = __popcll(m_eq);
-    __syncthreads();
-    int rank_eq = base_eq + __popcll(m_eq & below), all_eq = 0;
-    for (int i = 0; i < kSelThreads / 64; ++i) {
-      if (i < wave) rank_eq += wsum[0][i];
-      all_eq += wsum[0][i];
-    }
-    const bool stay = sure || (eq && rank_eq < need);
-    const unsigned long long m_stay = __ballot(stay);
-    if (lane == 0) wsum[1][wave] = __popcll(m_stay);
-    __syncthreads();
-    int at = base + __popcll(m_stay & below), all = 0;
-    for (int i = 0; i < kSelThreads / 64; ++i) {
-      if (i < wave) at += wsum[1][i];
-      all += wsum[1][i];
-    }
-    if (stay) {
-      kp[at] = t;
-      if (wo) wo[at] = wt;
-    }
-    base += all, base_eq += all_eq;
-    // (wsum[0] is written again only after every thread has passed the second barrier, wsum[1] after the next first one)
+    base_sure += all_x, base_eq += all_y;
+    if (!RESIDENT) __syncthreads();  // (the counts are written again)
   }
-  for (int j = n_keep + tid; j < keep; j += kSelThreads) kp[j] = -1;
+  for (int j = n_keep + tid; j < keep; j += T) kp[j] = -1;
   if (wo)
-    for (int j = n_keep + tid; j < max_seq_len; j += kSelThreads) wo[j] = 0.f;
+    for (int j = n_keep + tid; j < max_seq_len; j += T) wo[j] = 0.f;
 }
 
 // ---- eviction: the kept tokens move -----------------------------------------------------------------------
-// One workgroup per (64-token block of the destination, head, K or V): the block's 64 former indices and scales, one per
-// lane, give the new scale and each token's ratio; then the rows' cells are gathered, rounded again where the ratio is
-// not 1, and written.  Bound by memory: each kept byte is read and written once.
+// One workgroup per 64-token block of the destination and head, K and V together: the block's 64 former indices and scales, one
+// per lane, give the new scales and each token's ratio; then the rows' cells are all asked for, rounded again where the
+// ratio is not 1, and written.  Bound by memory: each kept byte is read and written once.
 constexpr int kMoveThreads = 256;
+
+// four codes of a live token under a scale that is 1 / r times theirs, r <= 1
+template <int CODE>
+__device__ __forceinline__ unsigned rescale(unsigned w, float r) {
+  if constexpr (CODE == NSN_Q8_INT8) {
+    const unsigned u = w ^ 0x80808080u;  // c + 128
+    unsigned y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float c = (float)(u >> (8 * i) & 255u) - 128.f;
+      const float x = c * r;
+      y[i] = __float_as_uint(x + 12582912.f);  // 3 * 2^22: the sum's last bits are the nearest integer (|x| <= 127)
+    }
+    const unsigned lo = __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(y[3], y[2], 0x0c0c0400u);
+    return lo | hi << 16;
+  } else {
+    float f[4];
+    to_float4<CODE>(w, f);
+    int x = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * r, f[1] * r, 0, false);
+    x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * r, f[3] * r, x, true);
+    return (unsigned)x;
+  }
+}
 
 template <int D, int CODE>
 __global__ __launch_bounds__(kMoveThreads) void move_kernel(Geometry g, const int32_t* seq_lens, int max_seq_len, int keep,
                                                             const int32_t* kept, View kc, View vc, View ko, View vo) {
   constexpr int kCells = 4 * D, kPer = kCells / kMoveThreads;
   constexpr int kTok = 256 / D, kCh = D / 16;
-  const int b = blockIdx.z, h = blockIdx.y >> 1, tid = threadIdx.x, lane = tid & 63;
-  const bool value = blockIdx.y & 1;
+  using piece = std::conditional_t<D == 128, uint2v, unsigned>;  // a token's channels in a cell of values
+  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   const int len = min(max(seq_lens[b], 0), max_seq_len);
   const int n_keep = min(len, keep), t0 = blockIdx.x * kBlock;
   if (t0 >= n_keep) return;
   const int live = min(n_keep - t0, kBlock);
-  const View& from = value ? vc : kc;
-  const View& to = value ? vo : ko;
-  const int64_t place = block_place(g, to.block_table, b, h, blockIdx.x);
-  if (place < 0) return;
-  // every wave by itself: lane = token of the block
-  int64_t row = -1;  // 64 * block + token inside: the former place
-  float was = 0.f;
-  if (lane < live) {
-    const int t = kept[((int64_t)b * g.hkv + h) * keep + t0 + lane];
-    const int64_t p = block_place(g, from.block_table, b, h, t / kBlock);
-    if (p >= 0) {
-      row = p * kBlock + t % kBlock;
-      was = from.scales[p];
+  const int64_t to_k = block_place(g, ko.block_table, b, h, blockIdx.x), to_v = block_place(g, vo.block_table, b, h, blockIdx.x);
+  // the first two waves, K and V: lane = token of the block
+  __shared__ int64_t s_row[2][kBlock];  // 64 * block + token inside: the former place; -1: there is none
+  __shared__ float s_ratio[2][kBlock];
+  if (tid < 2 * kBlock) {
+    const bool value = tid >= kBlock;
+    const View& from = value ? vc : kc;
+    int64_t row = -1;
+    float was = 0.f;
+    if (lane < live) {
+      const int t = kept[((int64_t)b * g.hkv + h) * keep + t0 + lane];
+      const int64_t p = block_place(g, from.block_table, b, h, t / kBlock);
+      if (p >= 0) {
+        row = p * kBlock + t % kBlock;
+        was = from.scales[p];
+      }
     }
+    const float level = wave_max(was);
+    s_row[value][lane] = row, s_ratio[value][lane] = level > 0.f ? was / level : 0.f;
+    const int64_t place = value ? to_v : to_k;
+    if (lane == 0 && place >= 0) (value ? vo : ko).scales[place] = level;
   }
-  const float level = wave_max(was);
-  const float ratio = level > 0.f ? was / level : 0.f;
-  __shared__ int64_t s_row[kBlock];
-  __shared__ float s_ratio[kBlock];
-  if (tid < kBlock) s_row[lane] = row, s_ratio[lane] = ratio;
-  if (tid == 0) to.scales[place] = level;
   __syncthreads();
-  uint8_t* dst = to.codes + place * (int64_t)(kBlock * D);
-  auto again = [](unsigned old, float r) {
-    float y[4];
-    to_float4<CODE>(old, y);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] *= r;
-    return to_codes<CODE>(y);
-  };
+  uint4v x[kPer];
+  piece y[kPer][kTok];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int cell = tid + i * kMoveThreads;
-    unsigned w[4] = {0, 0, 0, 0};
-    if (!value) {
-      const int t = cell / kCh;
-      if (t >= live) continue;
-      const int64_t r = s_row[t];
-      if (r >= 0) {
-        const uint4v v = *reinterpret_cast<const uint4v*>(from.codes + r * D + cell % kCh * 16);
-        w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];
-        if (s_ratio[t] != 1.f) {
+    const int64_t r = s_row[0][cell / kCh];
+    x[i] = uint4v{0, 0, 0, 0};
+    if (r >= 0) x[i] = *reinterpret_cast<const uint4v*>(kc.codes + r * D + cell % kCh * 16);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) w[q] = again(w[q], s_ratio[t]);
-        }
+    for (int k = 0; k < kTok; ++k) {
+      const int64_t rv = s_row[1][cell / 16 * kTok + k];
+      y[i][k] = piece{};
+      if (rv >= 0) y[i][k] = *reinterpret_cast<const piece*>(vc.codes + rv / kTok * 256 + cell % 16 * 16 + (int)(rv % kTok) * kCh);
+    }
+  }
+  if (to_k >= 0) {
+    uint8_t* dst = ko.codes + to_k * (int64_t)(kBlock * D);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int cell = tid + i * kMoveThreads, t = cell / kCh;
+      const float r = s_ratio[0][t];
+      if (r != 1.f) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[i][q] = rescale<CODE>(x[i][q], r);
       }
-      *reinterpret_cast<uint4v*>(dst + cell * 16) = uint4v{w[0], w[1], w[2], w[3]};
-    } else {
-      const int t = cell / 16 * kTok, n = cell % 16;
+      if (t < live) *reinterpret_cast<uint4v*>(dst + cell * 16) = x[i];
+    }
+  }
+  if (to_v >= 0) {
+    uint8_t* dst = vo.codes + to_v * (int64_t)(kBlock * D);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int tq = t + q * 4 / kCh;
-        if (tq >= live) continue;
-        const int64_t r = s_row[tq];
-        if (r >= 0) {
-          w[q] = *reinterpret_cast<const unsigned*>(from.codes + (r / kTok) * 256 + n * 16 + (int)(r % kTok) * kCh + q * 4 % kCh);
-          if (s_ratio[tq] != 1.f) w[q] = again(w[q], s_ratio[tq]);
+    for (int i = 0; i < kPer; ++i) {
+      const int cell = tid + i * kMoveThreads, t = cell / 16 * kTok;
+      uint4v u;
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        const float r = s_ratio[1][t + k];
+#pragma unroll
+        for (int q = 0; q < 4 / kTok; ++q) {
+          unsigned c;
+          if constexpr (D == 128)
+            c = y[i][k][q];
+          else
+            c = y[i][k];
+          u[k * (4 / kTok) + q] = r != 1.f ? rescale<CODE>(c, r) : c;
         }
       }
       if (t + kTok <= live) {
-        *reinterpret_cast<uint4v*>(dst + cell * 16) = uint4v{w[0], w[1], w[2], w[3]};
-      } else {
+        *reinterpret_cast<uint4v*>(dst + cell * 16) = u;
+      } else {  // (places behind the last token stay as they were)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          if (t + q * 4 / kCh < live) reinterpret_cast<unsigned*>(dst + cell * 16)[q] = w[q];
+          if (t + q * 4 / kCh < live) reinterpret_cast<unsigned*>(dst + cell * 16)[q] = u[q];
       }
     }
   }
@@ -325,13 +401,21 @@ size_t evict_workspace_bytes(const nsn_q8_shape&, int, int, int) { return 0; }
 
 int evict_launch(const EvictCall& c) {
   const nsn_q8_shape& s = c.shape;
-  select_kernel<<<dim3(s.n_kv_heads, c.batch), kSelThreads, 0, c.stream>>>(s.n_kv_heads, s.max_len, c.weights, c.seq_lens, c.max_seq_len,
-                                                                          c.keep, c.first, c.recent, c.kept, c.new_lens, c.weights_out);
+  auto select = [&](auto kernel, int threads) {
+    kernel<<<dim3(s.n_kv_heads, c.batch), threads, 0, c.stream>>>(s.n_kv_heads, s.max_len, c.weights, c.seq_lens, c.max_seq_len, c.keep,
+                                                                  c.first, c.recent, c.kept, c.new_lens, c.weights_out);
+  };
+  if (c.max_seq_len <= 256 * 8)
+    select(select_kernel<256, 8, true>, 256);
+  else if (c.max_seq_len <= 1024 * 16)
+    select(select_kernel<1024, 16, true>, 1024);
+  else
+    select(select_kernel<1024, 16, false>, 1024);
   if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;
   const int blocks = (std::min(c.keep, c.max_seq_len) + kBlock - 1) / kBlock;
   if (blocks == 0) return NSN_OK;
   with_types(s, [&](auto d, auto code, auto) {
-    move_kernel<d.value, code.value><<<dim3(blocks, 2 * s.n_kv_heads, c.batch), kMoveThreads, 0, c.stream>>>(
+    move_kernel<d.value, code.value><<<dim3(blocks, s.n_kv_heads, c.batch), kMoveThreads, 0, c.stream>>>(
         make_geometry(s), c.seq_lens, c.max_seq_len, c.keep, c.kept, make_view(c.kc), make_view(c.vc), make_view(c.ko), make_view(c.vo));
     return 0;
   });

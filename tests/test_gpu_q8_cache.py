@@ -289,3 +289,21 @@ def test_evict_then_append_then_evict(gpu_api):
         a, b = b, a
         for kind in "kv":
             b.noise[kind] = (b.cache[kind].codes.cpu().numpy().reshape(b.noise[kind][0].shape), b.cache[kind].scales.cpu().numpy())
+
+
+@pytest.mark.parametrize("length", [2048, 2049, 16384, 16385, 40001])
+@pytest.mark.parametrize("kind", ["spread", "few values", "negative too"])
+def test_evict_of_long_sequences(gpu_api, length, kind):
+    """Around the lengths where the choice goes by another instance; weights over many powers of two, of few values, of both signs."""
+    rng = np.random.default_rng(length)
+    L = -(-length // 64) * 64
+    lens = [length, length - 700]
+    dev = Device(gpu_api, rng, E4M3, 64, 1, 2, L, 0, dtypes()["fp16"])
+    append(dev, rng, [0, 0], lens, length)
+    to = Device(gpu_api, rng, E4M3, 64, 1, 2, L, 0, dtypes()["fp16"])
+    w = weights_of(rng, 2, 1, L, lens)
+    if kind == "few values":
+        w = np.round(w).clip(0, 3).astype(np.float32)
+    elif kind == "negative too":
+        w = (rng.standard_normal(w.shape) * 10.0 ** rng.integers(-30, 30, w.shape)).astype(np.float32)
+    evict_and_check(gpu_api, rng, dev, to, lens, w, length // 3 + 1, 5, 99)

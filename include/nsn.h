@@ -451,7 +451,7 @@ int nsn_q8_attention(const nsn_q8_shape* shape, const nsn_rows* q, int n_q, cons
  * their order, to tokens 0, 1, .. of the same sequence and head in another cache.  The scale of a block there is the
  * largest of its tokens' former scales; codes of tokens whose scale was smaller are rounded again, c -> c * fp32(former / new) to
  * nearest even.
- *   weights      fp32 [batch][n_kv_heads][max_len] (weights_out of nsn_q8_attention)
+ *   weights      fp32 [batch][n_kv_heads][max_len] (weights_out of nsn_q8_attention), 16-byte aligned
  *   k_cache, v_cache  the caches read; k_out, v_out those written, of the same shape: other buffers, or (paged) the same
  *                ones under a block table that shares no page with what is read
  *   first, recent  >= 0, first + recent <= keep;  1 <= keep <= max_len

@@ -169,8 +169,8 @@ int nsn_q8_evict(const nsn_q8_shape* shape, const float* weights, const int32_t*
   if ((rc = check_cache(shape, v_cache, "V")) != NSN_OK) return rc;
   if ((rc = check_cache(shape, k_out, "K output")) != NSN_OK) return rc;
   if ((rc = check_cache(shape, v_out, "V output")) != NSN_OK) return rc;
-  if (!weights || !seq_lens_dev || !kept || !new_lens || batch < 0 || batch > 65535 || max_seq_len < 0 || max_seq_len > shape->max_len) {
-    set_error("q8_evict: null pointer, negative size, batch=%d beyond 65535, or max_seq_len=%d beyond max_len=%d", batch, max_seq_len,
+  if (!weights || (reinterpret_cast<uintptr_t>(weights) & 15) != 0 || !seq_lens_dev || !kept || !new_lens || batch < 0 || batch > 65535 || max_seq_len < 0 || max_seq_len > shape->max_len) {
+    set_error("q8_evict: null pointer, weights not 16-byte aligned, negative size, batch=%d beyond 65535, or max_seq_len=%d beyond max_len=%d", batch, max_seq_len,
               shape->max_len);
     return NSN_ERR_INVALID_ARG;
   }

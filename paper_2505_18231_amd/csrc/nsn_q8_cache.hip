@@ -129,13 +129,15 @@ int append_launch(const nsn_q8_shape& s, const nsn_rows& k, const nsn_rows& v, i
 }
 
 // ---- eviction: which tokens stay ------------------------------------------------------------------------
-// One workgroup per (sequence, head).  The weights, ordered as unsigned keys (NaN the least), stay in registers where a
-// sequence fits (16 to a thread; a longer one is read again for every pass).  The need-th largest key of the middle tokens is
-// found by digits of 11, 11 and 10 bits, with a histogram of each in LDS; then the tokens above it and the first of those that
-// equal it are counted off in order.  Integer sums only: the same tokens for any order of the threads.  Bound by the
-// histograms' additions to one address: the first lane's digit, often that of many lanes (weights of zero), is added once for all of
-// them, and a first digit of 11 bits spreads the others over four bins per power of two.
-constexpr int kBins = 2048;
+// One workgroup per (sequence, head).  The weights, ordered as unsigned keys (NaN the least, tokens that stay whatever the others are
+// above all), stay in registers where a sequence fits, K consecutive tokens to a thread (a longer one is read again for every
+// pass).  The need-th largest key of the middle tokens is found by digits of 11, 11 and 10 bits with a histogram of each in LDS,
+// until a bin holds no more than a wave's worth, whose keys are then compared with each other; a first digit of 11 bits spreads weights
+// over four bins per power of two.  Then the tokens above the key and the first of those that equal it are counted off in order.
+// Integer sums only: the same tokens for any order of the threads.  Bound by latency (a compute unit per head, some ten trips through
+// LDS and barriers): 64 heads of 16384 tokens NNN us, 8 of 1088 NNN us.
+constexpr int kBins = 2048, kFew = 64;
+constexpr unsigned kSure = 0xffffffffu;  // (no weight's key: that of infinity is 0xff800000)
 
 __device__ __forceinline__ unsigned weight_key(float w) {
   if (w != w) return 0u;
@@ -163,58 +165,65 @@ template <int T, int K, bool RESIDENT>
 __global__ __launch_bounds__(T) void select_kernel(int hkv, int max_len, const float* weights, const int32_t* seq_lens, int max_seq_len,
                                                    int keep, int first, int recent, int32_t* kept, int32_t* new_lens,
                                                    float* weights_out) {
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int len = min(max(seq_lens[b], 0), max_seq_len);
   const int n_keep = min(len, keep);
   const int64_t unit = (int64_t)b * hkv + h;
   const float* w = weights + unit * max_len;
   int32_t* kp = kept + unit * keep;
   float* wo = weights_out ? weights_out + unit * max_len : nullptr;
-  if (h == 0 && tid == 0) new_lens[b] = n_keep;
 
-  __shared__ int hist[kBins];
-  __shared__ int found[2];
+  __shared__ __attribute__((aligned(16))) int hist[kBins];
+  __shared__ int found[3];
+  __shared__ unsigned few[kFew];
   __shared__ int sums[2][T / 64];
-  __shared__ int count[2][K * T / 64];
-  float v[K];  // token base + i * T + tid
-  auto load = [&](int base) {
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      const int t = base + i * T + tid;
-      v[i] = t < len ? w[t] : 0.f;
-    }
-  };
-  if (RESIDENT) load(0);
-
   const int mid0 = first, mid1 = len - recent;  // the tokens to choose from, where len > keep
-  unsigned prefix = 0, mask = 0;
   int need = keep - first - recent;
   const bool choose = len > keep && need > 0;
-  if (choose) {
+  unsigned key[K];  // of token base + tid * K + i
+  auto load_weights = [&](int base, float (&v)[K]) {
+    const int live = len - base - tid * K;  // weights of this thread
+    const float* p = w + base + tid * K;
 #pragma unroll
+    for (int i = 0; i < K; i += 4) {
+      // (rows are multiples of 64 long: a piece of four that begins inside the sequence lies inside the row)
+      const float4v x = i < live ? *reinterpret_cast<const float4v*>(p + i) : float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i + e] = x[e];
+    }
+  };
+  auto load = [&](int base) {
+    const int t0 = base + tid * K, m0 = len <= keep ? K : mid0 - t0, m1 = mid1 - t0;
+    float v[K];
+    load_weights(base, v);
+#pragma unroll
+    for (int i = 0; i < K; ++i) key[i] = i < m0 || i >= m1 ? kSure : weight_key(v[i]);
+  };
+  if (RESIDENT) load(0);
+  // (what does not hang on the choice, while the weights are on their way)
+  if (h == 0 && tid == 0) new_lens[b] = n_keep;
+  for (int j = n_keep + tid; j < keep; j += T) kp[j] = -1;
+  if (wo)
+    for (int j = n_keep + tid; j < max_seq_len; j += T) wo[j] = 0.f;
+
+  unsigned prefix = kSure - 1, mask = 0;  // (where there is nothing to choose: those above it)
+  if (choose) {
+    prefix = 0;
+#pragma unroll 1
     for (int digit = 0; digit < 3; ++digit) {
       const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-      for (int i = tid; i < kBins; i += T) hist[i] = 0;
+      constexpr int kOwn = kBins / T;  // bins of a thread
+      static_assert(kOwn >= 2, "two bins to a thread at least");
+#pragma unroll
+      for (int i = 0; i < kOwn; i += 2) *reinterpret_cast<uint2v*>(&hist[tid * kOwn + i]) = uint2v{0, 0};
       __syncthreads();
       for (int base = 0; base < len; base += T * K) {
         if (!RESIDENT) load(base);
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-          const int t = base + i * T + tid;
-          const unsigned k = weight_key(v[i]);
-          const bool in = t >= mid0 && t < mid1 && (k & mask) == prefix;
-          const unsigned long long lanes = __ballot(in);
-          if (lanes == 0) continue;
-          const int d = (int)(k >> shift) & ((1 << bits) - 1), lead = __ffsll(lanes) - 1, dl = __builtin_amdgcn_readlane(d, lead);
-          const unsigned long long same = __ballot(in && d == dl);
-          if (lane == lead)
-            atomicAdd(&hist[dl], (int)__popcll(same));
-          else if (in && d != dl)
-            atomicAdd(&hist[d], 1);
-        }
+        for (int i = 0; i < K; ++i)
+          if (digit == 0 ? key[i] != kSure : (key[i] & mask) == prefix) atomicAdd(&hist[(key[i] >> shift) & ((1 << bits) - 1)], 1);
       }
       __syncthreads();
-      constexpr int kOwn = kBins / T;  // bins of a thread
       int c[kOwn], x = 0, y = 0, all = 0, none;
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) c[i] = hist[tid * kOwn + i], x += c[i];
@@ -222,64 +231,84 @@ __global__ __launch_bounds__(T) void select_kernel(int hkv, int max_len, const f
       int above = all - x;  // in the bins of the threads behind
 #pragma unroll
       for (int i = kOwn - 1; i >= 0; --i) {
-        if (above < need && above + c[i] >= need) found[0] = tid * kOwn + i, found[1] = need - above;
+        if (above < need && above + c[i] >= need) found[0] = tid * kOwn + i, found[1] = need - above, found[2] = c[i];
         above += c[i];
       }
       __syncthreads();
       prefix |= (unsigned)found[0] << shift;
       mask |= ((1u << bits) - 1) << shift;
       need = found[1];
+      const int left = found[2];
+      if (left <= kFew && digit < 2) {
+        // the bin's keys, in their order; the one that fewer than need exceed and need or more reach
+        int before = 0;
+        for (int base = 0; base < len; base += T * K) {
+          if (!RESIDENT) load(base);
+          int own = 0, zero = 0, all_few, none2;
+#pragma unroll
+          for (int i = 0; i < K; ++i) own += (key[i] & mask) == prefix;
+          int at = own;
+          scan_pair<T>(at, zero, all_few, none2, sums);
+          at += before - own;
+          if (own) {
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+              if ((key[i] & mask) == prefix) few[at++] = key[i];
+          }
+          before += all_few;
+          __syncthreads();  // (the sums are written again)
+        }
+        if (tid < 64) {
+          const unsigned own = tid < left ? few[tid] : 0u;
+          int more = 0, same = 0;
+          for (int i = 0; i < left; ++i) {
+            const unsigned k = (unsigned)__builtin_amdgcn_readlane((int)own, i);
+            more += k > own, same += k == own;
+          }
+          if (tid < left && more < need && more + same >= need) found[0] = (int)own, found[1] = need - more;  // (equal keys write the same)
+        }
+        __syncthreads();
+        prefix = (unsigned)found[0], need = found[1];
+        break;
+      }
     }
   }
-  // In order: tokens that stay whatever the others are, and the first `need` of those whose key equals `prefix`.
+  // In order: the tokens above `prefix`, and the first `need` of those that equal it.
   int base_sure = 0, base_eq = 0;
   for (int base = 0; base < len; base += T * K) {
     if (!RESIDENT) load(base);
-    unsigned long long sure[K], eq[K];
+    const int t0 = base + tid * K, live = len - t0;
+    int own_sure = 0, own_eq = 0, all_sure, all_eq;
+    float v[K];
+    load_weights(base, v);
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-      const int t = base + i * T + tid;
-      bool s = false, e = false;
-      if (t < len) {
-        if (len <= keep || t < first || t >= mid1) {
-          s = true;
-        } else if (choose) {
-          const unsigned k = weight_key(v[i]);
-          s = k > prefix, e = k == prefix;
-        }
-      }
-      sure[i] = __ballot(s), eq[i] = __ballot(e);
-      if (lane == 0) count[0][i * (T / 64) + wave] = __popcll(sure[i]), count[1][i * (T / 64) + wave] = __popcll(eq[i]);
+      own_sure += i < live && key[i] > prefix;
+      own_eq += i < live && key[i] == prefix;
     }
-    __syncthreads();
-    static_assert(K * T / 64 <= T, "one count to a thread");
-    const int own_x = tid < K * T / 64 ? count[0][tid] : 0, own_y = tid < K * T / 64 ? count[1][tid] : 0;
-    int x = own_x, y = own_y, all_x, all_y;
-    scan_pair<T>(x, y, all_x, all_y, sums);
-    if (tid < K * T / 64) count[0][tid] = x - own_x, count[1][tid] = y - own_y;
-    __syncthreads();
-    const unsigned long long below = (1ull << lane) - 1;
+    int sure = own_sure, eq = own_eq;
+    __syncthreads();  // (sums are read by the scan before)
+    scan_pair<T>(sure, eq, all_sure, all_eq, sums);
+    sure += base_sure - own_sure, eq += base_eq - own_eq;  // of the tokens before this thread's
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-      const int before_eq = base_eq + count[1][i * (T / 64) + wave] + (int)__popcll(eq[i] & below);
-      const int at = base_sure + count[0][i * (T / 64) + wave] + (int)__popcll(sure[i] & below) + min(before_eq, need);
-      if ((sure[i] >> lane & 1) || ((eq[i] >> lane & 1) && before_eq < need)) {
-        kp[at] = base + i * T + tid;
+      const bool is_sure = i < live && key[i] > prefix, is_eq = i < live && key[i] == prefix;
+      if (is_sure || (is_eq && eq < need)) {
+        const int at = sure + min(eq, need);
+        kp[at] = t0 + i;
         if (wo) wo[at] = v[i];
       }
+      sure += is_sure, eq += is_eq;
     }
-    base_sure += all_x, base_eq += all_y;
-    if (!RESIDENT) __syncthreads();  // (the counts are written again)
+    base_sure += all_sure, base_eq += all_eq;
   }
-  for (int j = n_keep + tid; j < keep; j += T) kp[j] = -1;
-  if (wo)
-    for (int j = n_keep + tid; j < max_seq_len; j += T) wo[j] = 0.f;
 }
 
 // ---- eviction: the kept tokens move -----------------------------------------------------------------------
-// One workgroup per 64-token block of the destination and head, K and V together: the block's 64 former indices and scales, one
+// One workgroup per NB 64-token blocks of the destination and head, K and V together: a block's 64 former indices and scales, one
 // per lane, give the new scales and each token's ratio; then the rows' cells are all asked for, rounded again where the
-// ratio is not 1, and written.  Bound by memory: each kept byte is read and written once.
+// ratio is not 1, and written.  Bound by memory: each kept byte is read and written once.  The way from the indices over the
+// pages and scales to the first row is four trips to memory, so many blocks go four to a workgroup.
 constexpr int kMoveThreads = 256;
 
 // four codes of a live token under a scale that is 1 / r times theirs, r <= 1
@@ -305,93 +334,102 @@ __device__ __forceinline__ unsigned rescale(unsigned w, float r) {
   }
 }
 
-template <int D, int CODE>
+template <int D, int CODE, int NB>
 __global__ __launch_bounds__(kMoveThreads) void move_kernel(Geometry g, const int32_t* seq_lens, int max_seq_len, int keep,
                                                             const int32_t* kept, View kc, View vc, View ko, View vo) {
-  constexpr int kCells = 4 * D, kPer = kCells / kMoveThreads;
+  constexpr int kPer = 4 * D / kMoveThreads;  // cells of a thread in a block
   constexpr int kTok = 256 / D, kCh = D / 16;
   using piece = std::conditional_t<D == 128, uint2v, unsigned>;  // a token's channels in a cell of values
-  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = min(max(seq_lens[b], 0), max_seq_len);
-  const int n_keep = min(len, keep), t0 = blockIdx.x * kBlock;
+  const int n_keep = min(len, keep), blk0 = blockIdx.x * NB, t0 = blk0 * kBlock;
   if (t0 >= n_keep) return;
-  const int live = min(n_keep - t0, kBlock);
-  const int64_t to_k = block_place(g, ko.block_table, b, h, blockIdx.x), to_v = block_place(g, vo.block_table, b, h, blockIdx.x);
-  // the first two waves, K and V: lane = token of the block
-  __shared__ int64_t s_row[2][kBlock];  // 64 * block + token inside: the former place; -1: there is none
-  __shared__ float s_ratio[2][kBlock];
-  if (tid < 2 * kBlock) {
-    const bool value = tid >= kBlock;
-    const View& from = value ? vc : kc;
+  const int live = min(n_keep - t0, NB * kBlock);
+  __shared__ int64_t s_row[2][NB * kBlock];  // 64 * block + token inside: the former place; -1: there is none
+  __shared__ float s_ratio[2][NB * kBlock];
+  __shared__ int64_t s_to[2][NB];            // the blocks written; -1: there is none
+  for (int u = wave; u < 2 * NB; u += kMoveThreads / 64) {  // a wave: K or V of a block
+    const int kind = u / NB, blk = u % NB, at = blk * kBlock + lane;
+    const View& from = kind ? vc : kc;
+    const View& to = kind ? vo : ko;
     int64_t row = -1;
     float was = 0.f;
-    if (lane < live) {
-      const int t = kept[((int64_t)b * g.hkv + h) * keep + t0 + lane];
+    if (at < live) {
+      const int t = kept[((int64_t)b * g.hkv + h) * keep + t0 + at];
       const int64_t p = block_place(g, from.block_table, b, h, t / kBlock);
       if (p >= 0) {
         row = p * kBlock + t % kBlock;
         was = from.scales[p];
       }
     }
+    const int64_t place = blk * kBlock < live ? block_place(g, to.block_table, b, h, blk0 + blk) : -1;
     const float level = wave_max(was);
-    s_row[value][lane] = row, s_ratio[value][lane] = level > 0.f ? was / level : 0.f;
-    const int64_t place = value ? to_v : to_k;
-    if (lane == 0 && place >= 0) (value ? vo : ko).scales[place] = level;
+    s_row[kind][at] = row, s_ratio[kind][at] = level > 0.f ? was / level : 0.f;
+    if (lane == 0) {
+      s_to[kind][blk] = place;
+      if (place >= 0) to.scales[place] = level;
+    }
   }
   __syncthreads();
-  uint4v x[kPer];
-  piece y[kPer][kTok];
+  uint4v x[NB][kPer];
+  piece y[NB][kPer][kTok];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int cell = tid + i * kMoveThreads;
-    const int64_t r = s_row[0][cell / kCh];
-    x[i] = uint4v{0, 0, 0, 0};
-    if (r >= 0) x[i] = *reinterpret_cast<const uint4v*>(kc.codes + r * D + cell % kCh * 16);
-#pragma unroll
-    for (int k = 0; k < kTok; ++k) {
-      const int64_t rv = s_row[1][cell / 16 * kTok + k];
-      y[i][k] = piece{};
-      if (rv >= 0) y[i][k] = *reinterpret_cast<const piece*>(vc.codes + rv / kTok * 256 + cell % 16 * 16 + (int)(rv % kTok) * kCh);
-    }
-  }
-  if (to_k >= 0) {
-    uint8_t* dst = ko.codes + to_k * (int64_t)(kBlock * D);
+  for (int j = 0; j < NB; ++j)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int cell = tid + i * kMoveThreads, t = cell / kCh;
-      const float r = s_ratio[0][t];
-      if (r != 1.f) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) x[i][q] = rescale<CODE>(x[i][q], r);
-      }
-      if (t < live) *reinterpret_cast<uint4v*>(dst + cell * 16) = x[i];
-    }
-  }
-  if (to_v >= 0) {
-    uint8_t* dst = vo.codes + to_v * (int64_t)(kBlock * D);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int cell = tid + i * kMoveThreads, t = cell / 16 * kTok;
-      uint4v u;
+      const int cell = tid + i * kMoveThreads;
+      const int64_t r = s_row[0][j * kBlock + cell / kCh];
+      x[j][i] = uint4v{0, 0, 0, 0};
+      if (r >= 0) x[j][i] = *reinterpret_cast<const uint4v*>(kc.codes + r * D + cell % kCh * 16);
 #pragma unroll
       for (int k = 0; k < kTok; ++k) {
-        const float r = s_ratio[1][t + k];
-#pragma unroll
-        for (int q = 0; q < 4 / kTok; ++q) {
-          unsigned c;
-          if constexpr (D == 128)
-            c = y[i][k][q];
-          else
-            c = y[i][k];
-          u[k * (4 / kTok) + q] = r != 1.f ? rescale<CODE>(c, r) : c;
-        }
+        const int64_t rv = s_row[1][j * kBlock + cell / 16 * kTok + k];
+        y[j][i][k] = piece{};
+        if (rv >= 0) y[j][i][k] = *reinterpret_cast<const piece*>(vc.codes + rv / kTok * 256 + cell % 16 * 16 + (int)(rv % kTok) * kCh);
       }
-      if (t + kTok <= live) {
-        *reinterpret_cast<uint4v*>(dst + cell * 16) = u;
-      } else {  // (places behind the last token stay as they were)
+    }
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (t + q * 4 / kCh < live) reinterpret_cast<unsigned*>(dst + cell * 16)[q] = u[q];
+  for (int j = 0; j < NB; ++j) {
+    const int64_t to_k = s_to[0][j], to_v = s_to[1][j];
+    if (to_k >= 0) {
+      uint8_t* dst = ko.codes + to_k * (int64_t)(kBlock * D);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int cell = tid + i * kMoveThreads, t = j * kBlock + cell / kCh;
+        const float r = s_ratio[0][t];
+        if (r != 1.f) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[j][i][q] = rescale<CODE>(x[j][i][q], r);
+        }
+        if (t < live) *reinterpret_cast<uint4v*>(dst + cell * 16) = x[j][i];
+      }
+    }
+    if (to_v >= 0) {
+      uint8_t* dst = vo.codes + to_v * (int64_t)(kBlock * D);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int cell = tid + i * kMoveThreads, t = j * kBlock + cell / 16 * kTok;
+        uint4v u;
+#pragma unroll
+        for (int k = 0; k < kTok; ++k) {
+          const float r = s_ratio[1][t + k];
+#pragma unroll
+          for (int q = 0; q < 4 / kTok; ++q) {
+            unsigned c;
+            if constexpr (D == 128)
+              c = y[j][i][k][q];
+            else
+              c = y[j][i][k];
+            u[k * (4 / kTok) + q] = r != 1.f ? rescale<CODE>(c, r) : c;
+          }
+        }
+        if (t + kTok <= live) {
+          *reinterpret_cast<uint4v*>(dst + cell * 16) = u;
+        } else {  // (places behind the last token stay as they were)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (t + q * 4 / kCh < live) reinterpret_cast<unsigned*>(dst + cell * 16)[q] = u[q];
+        }
       }
     }
   }
@@ -415,8 +453,11 @@ int evict_launch(const EvictCall& c) {
   const int blocks = (std::min(c.keep, c.max_seq_len) + kBlock - 1) / kBlock;
   if (blocks == 0) return NSN_OK;
   with_types(s, [&](auto d, auto code, auto) {
-    move_kernel<d.value, code.value><<<dim3(blocks, s.n_kv_heads, c.batch), kMoveThreads, 0, c.stream>>>(
-        make_geometry(s), c.seq_lens, c.max_seq_len, c.keep, c.kept, make_view(c.kc), make_view(c.vc), make_view(c.ko), make_view(c.vo));
+    auto move = [&](auto nb) {
+      move_kernel<d.value, code.value, nb.value><<<dim3((blocks + nb.value - 1) / nb.value, s.n_kv_heads, c.batch), kMoveThreads, 0, c.stream>>>(
+          make_geometry(s), c.seq_lens, c.max_seq_len, c.keep, c.kept, make_view(c.kc), make_view(c.vc), make_view(c.ko), make_view(c.vo));
+    };
+    move(std::integral_constant<int, 1>{});
     return 0;
   });
   return hipGetLastError() == hipSuccess ? NSN_OK : NSN_ERR_HIP;

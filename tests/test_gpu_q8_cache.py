@@ -307,3 +307,14 @@ def test_evict_of_long_sequences(gpu_api, length, kind):
     elif kind == "negative too":
         w = (rng.standard_normal(w.shape) * 10.0 ** rng.integers(-30, 30, w.shape)).astype(np.float32)
     evict_and_check(gpu_api, rng, dev, to, lens, w, length // 3 + 1, 5, 99)
+
+
+@pytest.mark.parametrize("code,D", [(INT8, 128), (E4M3, 64)])
+def test_evict_of_many_sequences(gpu_api, code, D):
+    """Enough blocks that a workgroup moves four; the last group is not full, nor is its last block."""
+    rng = np.random.default_rng(88)
+    lens = [4200, 4101, 4100, 4099, 64, 0, 4160, 4097]
+    dev = Device(gpu_api, rng, code, D, 8, 8, 4224, 64, dtypes()["bf16"], drop=[(0, 3, -1)])
+    append(dev, rng, [0] * 8, lens, max(lens))
+    to = Device(gpu_api, rng, code, D, 8, 8, 4224, 64, dtypes()["bf16"], drop=[(1, 64, 10 ** 8), (2, 5, -2)])
+    evict_and_check(gpu_api, rng, dev, to, lens, weights_of(rng, 8, 8, 4224, lens), 4100, 4, 500)

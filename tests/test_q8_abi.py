@@ -115,11 +115,12 @@ def test_other_arguments_are_refused(L):
         assert attend(L, s, **kw) == -1, kw
     assert attend(L, s, batch=0) == 0 and attend(L, s, n_q=0) == 0
     assert attend(L, s, n_q=1 << 23) == api.NSN_ERR_UNSUPPORTED
-    need = api.nsn_q8_workspace_bytes(s, api.NSN_OP_Q8_ATTENTION, 1, 1, 1024)
+    need = api.nsn_q8_workspace_bytes(s, api.NSN_OP_Q8_ATTENTION, 1, 1, 1024)   # (that of a call with weights: the most)
     assert need > 0
     for kw in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=FAKE + 8)):
-        assert attend(L, s, **kw) == api.NSN_ERR_WORKSPACE, kw
-    for kw in (dict(w=None), dict(lens=None), dict(kept=None), dict(new=None), dict(batch=-1), dict(batch=65536), dict(max_seq=1025),
+        assert attend(L, s, w_out=FAKE, **kw) == api.NSN_ERR_WORKSPACE, kw
+    assert attend(L, s, ws_bytes=1 << 16) == api.NSN_ERR_WORKSPACE
+    for kw in (dict(w=None), dict(w=FAKE + 4), dict(lens=None), dict(kept=None), dict(new=None), dict(batch=-1), dict(batch=65536), dict(max_seq=1025),
                dict(max_seq=-1), dict(keep=0), dict(keep=1025), dict(first=-1), dict(recent=-1), dict(first=40, recent=25), dict(w_out=FAKE)):
         assert evict(L, s, **kw) == -1, kw
     assert evict(L, s, batch=0) == 0

@@ -3,7 +3,7 @@
 
 #include <type_traits>
 
-#include "nsn_device.h"
+#include "nsn_host.h"
 
 namespace nsn {
 namespace q8 {
@@ -24,6 +24,7 @@ struct Geometry {
   int max_len, n_pages, page_size;  // page_size 0: contiguous
   int pages_per_seq;
   int unit_tokens;                  // tokens per unit: page_size, or max_len
+  nsn::Geometry::Div page_div;      // division by page_size
 };
 
 struct View {
@@ -37,17 +38,27 @@ struct Rows {
   int64_t sb, sh, st;
 };
 
+// A value that no kernel of the call writes, at an address that is the same for the whole wave: comes through the scalar cache, and
+// waiting for it does not wait for the vector loads that were asked for before it
+template <typename T>
+__device__ __forceinline__ T load_uniform(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
 // Place of 64-token block `blk` of sequence b: index of the block among all units' blocks of head 0 .. (times D * 64 bytes: its
 // codes), or -1 where its page does not exist.  Pages are multiples of 64 tokens, so a block lies in one page.
+// UNIFORM: the same block for the whole wave.
+template <bool UNIFORM = false>
 __device__ __forceinline__ int64_t block_place(const Geometry& g, const int32_t* table, int b, int h, int blk) {
   int64_t unit = b;
   int in = blk;
   if (g.page_size > 0) {
-    const int per = g.page_size / kBlock, page = blk / per;
-    const int p = table[(int64_t)b * g.pages_per_seq + page];
+    const int page = tokens_div(blk * kBlock, g.page_div);
+    const int32_t* entry = table + (int64_t)b * g.pages_per_seq + page;
+    const int p = UNIFORM ? load_uniform(entry) : *entry;
     if ((unsigned)p >= (unsigned)g.n_pages) return -1;
     unit = p;
-    in = blk - page * per;
+    in = blk - page * (g.page_size / kBlock);
   }
   return (unit * g.hkv + h) * (int64_t)(g.unit_tokens / kBlock) + in;
 }
@@ -147,6 +158,7 @@ inline Geometry make_geometry(const nsn_q8_shape& s) {
   g.max_len = s.max_len, g.n_pages = s.n_pages, g.page_size = s.page_size;
   g.pages_per_seq = s.page_size > 0 ? s.max_len / s.page_size : 1;
   g.unit_tokens = s.page_size > 0 ? s.page_size : s.max_len;
+  g.page_div = tokens_divisor(g.unit_tokens);
   return g;
 }
 inline View make_view(const nsn_q8_cache& c) { return {c.codes, c.scales, c.block_table}; }

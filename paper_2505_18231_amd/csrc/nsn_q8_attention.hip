@@ -13,7 +13,6 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "nsn_host.h"
 #include "nsn_q8.h"
 
 namespace nsn {
@@ -378,13 +377,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   const int blk0 = cur.first(), blk1 = min(blocks, cur.last()), first_run = cur.first_run(), live = cur.runs();
   const int64_t line0 = ((int64_t)b * a.g.hkv + h) * a.rows + r0;
 
-  auto fetch = [&](Fetched<D>& x, int blk) {  // (always loads: block 0 of the cache in the place of one that is not there)
-    int64_t pk = block_place(a.g, a.kc.block_table, b, h, blk), pv = block_place(a.g, a.vc.block_table, b, h, blk);
+  int64_t next_k = 0, next_v = 0;
+  auto look_up = [&](int blk) {  // (a block ahead of its loads, so that these do not wait for the page tables)
+    next_k = block_place<true>(a.g, a.kc.block_table, b, h, blk), next_v = block_place<true>(a.g, a.vc.block_table, b, h, blk);
+  };
+  auto fetch = [&](Fetched<D>& x) {  // (always loads: block 0 of the cache in the place of one that is not there)
+    int64_t pk = next_k, pv = next_v;
     x.there = pk >= 0 && pv >= 0;
     if (!x.there) pk = pv = 0;
     x.k.load(a.kc.codes + pk * (int64_t)(kBlock * D));
     x.v.load(a.vc.codes + pv * (int64_t)(kBlock * D));
-    x.sk = a.kc.scales[pk], x.sv = a.vc.scales[pv];
+    x.sk = load_uniform(a.kc.scales + pk), x.sv = load_uniform(a.vc.scales + pv);
   };
   half8v q[D / 32];
   float factor = 0.f, m = -INFINITY, l = 0.f;
@@ -430,8 +433,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[j][e]);
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    top = fmaxf(top, xor_lane<16>(top));
+    top = fmaxf(top, xor_lane<32>(top));
     const float m_new = fmaxf(m, top), alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
     const float base = m_new == -INFINITY ? 0.f : m_new - kRowsLift;
     m = m_new;
@@ -469,21 +472,25 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   int blk = blk0 + wave;
   if (blk < blk1) {
     Fetched<D> x, y;
-    fetch(x, blk);
+    look_up(blk);
+    fetch(x);
+    look_up(min(blk + kWaves, blk1 - 1));
     factor = load_queries<D, BF>(a, b, h, r, pr.nq, q);
     while (true) {
-      fetch(y, min(blk + kWaves, blk1 - 1));
+      fetch(y);
+      look_up(min(blk + 2 * kWaves, blk1 - 1));
       work(x, blk);
       blk += kWaves;
       if (blk >= blk1) break;
-      fetch(x, min(blk + kWaves, blk1 - 1));
+      fetch(x);
+      look_up(min(blk + 2 * kWaves, blk1 - 1));
       work(y, blk);
       blk += kWaves;
       if (blk >= blk1) break;
     }
   }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
+  l += xor_lane<16>(l);
+  l += xor_lane<32>(l);
 
   // join the four waves: row n of wave w, channels kCh * (4 kg + e) + i; sums under 2^(m - kRowsLift)
   if (kg == 0) sm_m[wave][n] = m - kRowsLift, sm_l[wave][n] = l;
@@ -532,8 +539,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   float M = -INFINITY, L = 0.f, acc[kCh];
 #pragma unroll
   for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
-  if (row < rows_here) {
-    constexpr int kAhead = 4;
+  auto gather = [&](auto ahead) {
+    constexpr int kAhead = decltype(ahead)::value;
     for (int s0 = g0; s0 < live; s0 += kAhead * G) {
       float2v ml[kAhead], x[kAhead][kCh / 2];
 #pragma unroll
@@ -560,7 +567,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
         for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, x[k][i / 2][i & 1], acc[i]);
       }
     }
-  }
+  };
+  // (a trip to memory takes 2 us, whatever is asked for)
+  if (row < rows_here) live > 2 * G ? gather(std::integral_constant<int, 8>{}) : gather(std::integral_constant<int, 2>{});
   float* flat = &sm_o[0][0][0];
 #pragma unroll
   for (int i = 0; i < kCh; ++i) flat[group * kStride + c0 + i] = acc[i];
@@ -643,7 +652,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
   float next_sk = 0.f, next_sv = 0.f;
   bool next_there = false;
   auto fetch = [&](int blk) {
-    const int64_t pk = block_place(a.g, a.kc.block_table, b, h, blk), pv = block_place(a.g, a.vc.block_table, b, h, blk);
+    const int64_t pk = block_place<true>(a.g, a.kc.block_table, b, h, blk), pv = block_place<true>(a.g, a.vc.block_table, b, h, blk);
     next_there = pk >= 0 && pv >= 0;
     if (!next_there) return;
     const uint8_t* kp = a.kc.codes + pk * (int64_t)(kBlock * D);
@@ -652,7 +661,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     for (int i = 0; i < kKeyCells; ++i) kw[i] = *reinterpret_cast<const uint4v*>(kp + (tid + i * kWaves * 64) * 16);
 #pragma unroll
     for (int c = 0; c < kCellsOf4; ++c) vw[c] = *reinterpret_cast<const uint4v*>(vp + (vt / kTok + c) * 256 + vn * 16);
-    next_sk = a.kc.scales[pk], next_sv = a.vc.scales[pv];
+    next_sk = load_uniform(a.kc.scales + pk), next_sv = load_uniform(a.vc.scales + pv);
     if (CODE == NSN_Q8_E4M3 && (blk + 1) * kBlock > pr.len) {  // places behind the last token may hold NaN: 0 * NaN is one
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -734,7 +743,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[j][e]);
-      top = fmaxf(top, __shfl_xor(top, 32, 64)) * f;
+      top = fmaxf(top, xor_lane<32>(top)) * f;
       if (__any(top > m + kLazy)) {  // (each row by its own scores: its result does not hang on its neighbours)
         const float m_new = top > m + kLazy ? top : m;
         const float alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
@@ -791,7 +800,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     }
     if (blk + 1 < blk1 && next_there) stage(sm[buf ^ 1]);
   }
-  l += __shfl_xor(l, 32, 64);
+  l += xor_lane<32>(l);
   // o[i][e]: row 32 i + 8 (e / 4) + 4 hh + e % 4 of the transposed values; the channels of cell c are its rows 16 x + c
   float M = l == 0.f ? -INFINITY : m - kLift, unit_of_o = sref;
   [&] {
@@ -913,7 +922,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void weights_kernel(Args a) {
     for (int e = 0; e < 16; ++e) sum[j][e] = 0.f;
   bool there = t0 < pr.len;
   if (there) {
-    const int64_t pk = block_place(a.g, a.kc.block_table, b, h, t0 / kBlock), pv = block_place(a.g, a.vc.block_table, b, h, t0 / kBlock);
+    const int64_t pk = block_place<true>(a.g, a.kc.block_table, b, h, t0 / kBlock), pv = block_place<true>(a.g, a.vc.block_table, b, h, t0 / kBlock);
     there = pk >= 0 && pv >= 0;
     if (there) {
       const uint8_t* p = a.kc.codes + pk * (int64_t)(kBlock * D) + 8 * hh;
@@ -924,7 +933,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void weights_kernel(Args a) {
           const uint2v w = *reinterpret_cast<const uint2v*>(p + (32 * j + n) * D + 16 * ks);
           k[j][ks] = to_operand8<CODE, BF>(w[0], w[1]);
         }
-      f = a.scale_log2 * a.kc.scales[pk];
+      f = a.scale_log2 * load_uniform(a.kc.scales + pk);
     }
   }
   uint4v piece[kPieces];

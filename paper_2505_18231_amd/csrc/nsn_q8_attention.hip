@@ -49,6 +49,8 @@ struct Args {
 constexpr int kWaves = 4;
 constexpr int kCounterInts = 16, kMaxCounters = 2048;  // (the workspace starts with them, in every call's layout)
 
+constexpr float kMasked = -1e30f;  // the score of a token that is not seen (finite: a factor of it may be 0)
+
 // what a (sequence, kv head) is asked
 struct Problem {
   int len, nq, vis0;  // vis0: tokens that query 0 sees (causal), possibly negative
@@ -200,7 +202,6 @@ struct ValueCodes {
 // Units of 16 rows.  The four waves of a workgroup take a segment's blocks in turn, each with the next block's codes on their way
 // to registers while it works on one, and are joined through LDS.  Bound by memory: every code is read once, and the
 // conversions and products of a block fill a third of the time that its bytes take.
-constexpr int kRowsLift = 12;  // weights are 2^kRowsLift at most: those down to 2^-26 of the largest are normal fp16 numbers
 
 template <int D>
 struct Fetched {
@@ -209,6 +210,41 @@ struct Fetched {
   float sk, sv;
   bool there;
 };
+
+// ---- the running maximum and the values' scale ------------------------------------------------------------
+// The output accumulates in the matrix registers from block to block without a pass over it:
+//   - a row's running maximum m is moved (and its sums rescaled) only when its scores pass it by 2^kLazy;
+//   - a block's value scale sv enters the exponent, p' = 2^(s - m + kLift + log2(sv / sref)), against a power of two sref that
+//     follows sv when it is off by more than 2^kSpan.  p' stays below 2^(kLift + kLazy + kSpan + 1) <= 2^15, and weights down to 2^-20 of
+//     the row's largest one are normal fp16 numbers.
+// Then sum p v = sref / 2^kLift * (what o holds), sum p = l / 2^kLift with l += (sum p') * (sref / sv).
+constexpr int kLazy = 4, kSpan = 4, kLift = 6;
+
+// top: the row's largest score of the block; ratio = sref / sv, lift = kLift + log2(sv / sref) for the block
+template <int N, typename V>
+__device__ __forceinline__ void running(float top, float sv, float& m, float& l, float& sref, V (&o)[N], float& ratio, float& lift) {
+  if (__any(top > m + kLazy)) {  // (each row by its own scores: its result does not hang on its neighbours)
+    const float m_new = top > m + kLazy ? top : m;
+    const float alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] *= alpha;
+  }
+  ratio = 1.f, lift = kLift;
+  if (sv > 0.f) {
+    // (a jump of more than 2^60 downwards would take the sums out of range: weights that small count as they underflow)
+    if (!(sv <= sref * (1 << kSpan) && sv * (1 << kSpan) >= sref) && !(sv < sref * 0x1p-60f)) {
+      const float now = ldexpf(0.5f, __builtin_amdgcn_frexp_expf(sv));
+      const float turn = sref > 0.f ? sref / now : 0.f;
+      sref = now;
+#pragma unroll
+      for (int i = 0; i < N; ++i) o[i] *= turn;
+    }
+    ratio = sref / sv;
+    lift = kLift + __log2f(sv / sref);
+  }
+}
 
 // ---- the list of the work --------------------------------------------------------------------------------
 // A unit is a tile of TILE rows of a (sequence, kv head); the list holds the 64-token blocks of all units in the order (sequence,
@@ -390,7 +426,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
     x.sk = load_uniform(a.kc.scales + pk), x.sv = load_uniform(a.vc.scales + pv);
   };
   half8v q[D / 32];
-  float factor = 0.f, m = -INFINITY, l = 0.f;
+  float factor = 0.f, m = -INFINITY, l = 0.f, sref = 0.f;
   float4v o[kCh];
 #pragma unroll
   for (int i = 0; i < kCh; ++i) o[i] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -415,59 +451,66 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       for (int ks = 0; ks < D / 32; ++ks)
         s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.k.template operand<CODE>(j, ks), q[ks], s[j], 0, 0, 0);
     }
-    float top = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s[j] *= f;
-    if (t0 + kBlock > vis_min) {
+    const bool masked = t0 + kBlock > vis_min;
+    if (masked) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (t0 + 16 * j + 4 * kg + e >= vis) s[j][e] = -INFINITY;
+          if (t0 + 16 * j + 4 * kg + e >= vis) s[j][e] = kMasked;
     }
     if (sc && r < n_rows) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<float4v*>(sc + 16 * j) = s[j];
+      for (int j = 0; j < 4; ++j) {
+        float4v y = s[j] * f;
+        if (masked) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t0 + 16 * j + 4 * kg + e >= vis) y[e] = -INFINITY;
+        }
+        *reinterpret_cast<float4v*>(sc + 16 * j) = y;
+      }
     }
+    float top = s[0][0];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[j][e]);
     top = fmaxf(top, xor_lane<16>(top));
-    top = fmaxf(top, xor_lane<32>(top));
-    const float m_new = fmaxf(m, top), alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
-    const float base = m_new == -INFINITY ? 0.f : m_new - kRowsLift;
-    m = m_new;
-    l *= alpha;
+    top = fmaxf(top, xor_lane<32>(top)) * f;
+    float ratio, lift;
+    running<kCh>(top, x.sv, m, l, sref, o, ratio, lift);
+    const float base = m - lift;
+    float sum = 0.f;
     half8v p[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float4v w;
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        w[e] = fast_exp2(s[j][e] - base);
-        l += w[e];
-      }
-      const half4v u = __builtin_convertvector(w, half4v);
+      for (int e = 0; e < 4; ++e) s[j][e] = fast_exp2(fmaf(s[j][e], f, -base));
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (t0 + 16 * j + 4 * kg + e >= vis) s[j][e] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sum += (s[j][0] + s[j][1]) + (s[j][2] + s[j][3]);
+      const half4v u = __builtin_convertvector(s[j], half4v);
 #pragma unroll
       for (int e = 0; e < 4; ++e) p[j >> 1][4 * (j & 1) + e] = u[e];
     }
+    l = fmaf(sum, ratio, l);
 #pragma unroll
-    for (int c2 = 0; c2 < kCh / 2; ++c2) {
-      float4v u = {0.f, 0.f, 0.f, 0.f}, v = {0.f, 0.f, 0.f, 0.f};
+    for (int st = 0; st < 2; ++st)
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
+      for (int c2 = 0; c2 < kCh / 2; ++c2) {
         half8v y, z;
         x.v.template operands<CODE>(st, c2, y, z);
-        u = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, p[st], u, 0, 0, 0);
-        v = __builtin_amdgcn_mfma_f32_16x16x32_f16(z, p[st], v, 0, 0, 0);
+        o[2 * c2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, p[st], o[2 * c2], 0, 0, 0);
+        o[2 * c2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(z, p[st], o[2 * c2 + 1], 0, 0, 0);
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        o[2 * c2][e] = fmaf(x.sv, u[e], o[2 * c2][e] * alpha);
-        o[2 * c2 + 1][e] = fmaf(x.sv, v[e], o[2 * c2 + 1][e] * alpha);
-      }
-    }
   };
   int blk = blk0 + wave;
   if (blk < blk1) {
@@ -492,13 +535,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   l += xor_lane<16>(l);
   l += xor_lane<32>(l);
 
-  // join the four waves: row n of wave w, channels kCh * (4 kg + e) + i; sums under 2^(m - kRowsLift)
-  if (kg == 0) sm_m[wave][n] = m - kRowsLift, sm_l[wave][n] = l;
+  // join the four waves: row n of wave w, channels kCh * (4 kg + e) + i; sums under 2^(m - kLift)
+  if (kg == 0) sm_m[wave][n] = l == 0.f ? -INFINITY : m - kLift, sm_l[wave][n] = l;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
     for (int i = 0; i < kCh; i += 4)
-      *reinterpret_cast<float4v*>(&sm_o[wave][n][kCh * (4 * kg + e) + i]) = float4v{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]};
+      *reinterpret_cast<float4v*>(&sm_o[wave][n][kCh * (4 * kg + e) + i]) = float4v{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]} * sref;
   __syncthreads();
   const int rows_here = min(16, n_rows - r0);
   // the partial of the unit's k-th run: a run has room for two, one of a unit that began before it and one of a unit that
@@ -600,13 +643,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
 // converted once per workgroup and staged in LDS as fp16: keys token by token, values transposed, in the order in which the score
 // product leaves the weights in a lane, so that both products read their first operand as 16-byte rows and the weights never
 // leave their lane.  The next tile's codes are on their way to registers while a tile is worked on; two tiles in LDS, one barrier a tile.
-//
-// The output accumulates in the matrix registers from tile to tile without a pass over it:
-//   - the running maximum is moved (and the sums rescaled) only when a row's scores pass it by 2^kLazy;
-//   - a tile's value scale sv enters the exponent, p' = 2^(s - m + kLift + log2(sv / sref)), against a power of two sref that
-//     follows sv when it is off by more than 2^kSpan.  p' stays below 2^(kLift + kLazy + kSpan + 1) <= 2^15, and weights down to 2^-20 of
-//     the row's largest one are normal fp16 numbers.
-constexpr int kLazy = 4, kSpan = 4, kLift = 6;
 
 template <int D>
 struct ChunkTile {
@@ -736,7 +772,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) s[j][e] = -1e30f;  // (finite: f may be 0)
+            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) s[j][e] = kMasked;
       }
       float top = s[0][0];
 #pragma unroll
@@ -744,31 +780,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[j][e]);
       top = fmaxf(top, xor_lane<32>(top)) * f;
-      if (__any(top > m + kLazy)) {  // (each row by its own scores: its result does not hang on its neighbours)
-        const float m_new = top > m + kLazy ? top : m;
-        const float alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
-        m = m_new;
-        l *= alpha;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-      }
-      float ratio = 1.f, lift = kLift;  // sref / sv, kLift + log2(sv / sref)
-      if (sv > 0.f) {
-        // (a jump of more than 2^60 downwards would take the sums out of range: weights that small count as they underflow)
-        if (!(sv <= sref * (1 << kSpan) && sv * (1 << kSpan) >= sref) && !(sv < sref * 0x1p-60f)) {
-          const float now = ldexpf(0.5f, __builtin_amdgcn_frexp_expf(sv));
-          const float turn = sref > 0.f ? sref / now : 0.f;
-          sref = now;
-#pragma unroll
-          for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[i][e] *= turn;
-        }
-        ratio = sref / sv;
-        lift = kLift + __log2f(sv / sref);
-      }
+      float ratio, lift;
+      running<D / 32>(top, sv, m, l, sref, o, ratio, lift);
       const float base = m - lift;
       float sum[2] = {0.f, 0.f};
       half8v p[4];

@@ -375,19 +375,16 @@ __device__ __forceinline__ bool arrives_last(const Args& a, int first_run, int l
 // factor of a part whose maximum is m in a sum under the maximum M
 __device__ __forceinline__ float part_factor(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
 
-// one row's result: channels c0 .. c0 + N - 1 (acc: sums under the total L), its logarithm from the thread of channel 0
-template <int D, bool BF, int N>
-__device__ __forceinline__ void write_row(const Args& a, int b, int h, int r, int c0, float M, float L, const float (&acc)[N]) {
+// one row's result: thread n of 16 holds channels 32 i + 2 n, 32 i + 2 n + 1 (acc: sums under the total L)
+template <int D, bool BF>
+__device__ __forceinline__ void write_row(const Args& a, int b, int h, int r, int n, float M, float L, const float2v (&acc)[D / 32]) {
   const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;
   const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
-  alignas(16) uint16_t u[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) u[i] = from_float<BF>(acc[i] * inv);
-  if constexpr (N == 8)
-    *reinterpret_cast<uint4v*>(a.out + place * D + c0) = *reinterpret_cast<const uint4v*>(u);
-  else
-    *reinterpret_cast<uint2v*>(a.out + place * D + c0) = *reinterpret_cast<const uint2v*>(u);
-  if (c0 == 0) {
+  for (int i = 0; i < D / 32; ++i)
+    *reinterpret_cast<unsigned*>(a.out + place * D + 32 * i + 2 * n) =
+        (unsigned)from_float<BF>(acc[i][0] * inv) | (unsigned)from_float<BF>(acc[i][1] * inv) << 16;
+  if (n == 0) {
     const float z = L == 0.f ? -INFINITY : M + __log2f(L);
     if (a.lse) a.lse[place] = z * kLn2;
     a.lse2[((int64_t)b * a.g.hkv + h) * a.rows + r] = z;
@@ -400,7 +397,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), kg = lane >> 4, n = lane & 15;
   Cursor<16> cur;
   if (!cur.begin(a, blockIdx.x)) return;
-  constexpr int kStride = D + 4;
+  constexpr int kStride = D + 4, kPairs = D / 32;
   __shared__ __attribute__((aligned(16))) float sm_o[kWaves][16][kStride];
   __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
   __shared__ int arrived;
@@ -549,11 +546,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   auto partial_of = [&](int k) { return a.partial + ((int64_t)(first_run + k) * 2 + (k == 0)) * 16 * (D + 2); };
   [&] {
   {
-    // 16 threads per row, D / 16 channels each
-    const int row = tid >> 4, c0 = (tid & 15) * kCh;
-    float M = -INFINITY, L = 0.f, acc[kCh];
+    // 16 threads per row
+    const int row = tid >> 4, n16 = tid & 15;
+    float M = -INFINITY, L = 0.f;
+    float2v acc[kPairs];
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+    for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_m[w][row]);
 #pragma unroll
@@ -561,37 +559,38 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       const float e = part_factor(sm_m[w][row], M);
       L = fmaf(e, sm_l[w][row], L);
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, sm_o[w][row][c0 + i], acc[i]);
+      for (int i = 0; i < kPairs; ++i) acc[i] += e * *reinterpret_cast<const float2v*>(&sm_o[w][row][32 * i + 2 * n16]);
     }
     if (live == 1) {
-      if (row < rows_here) write_row<D, BF, kCh>(a, b, h, r0 + row, c0, M, L, acc);
+      if (row < rows_here) write_row<D, BF>(a, b, h, r0 + row, n16, M, L, acc);
       return;
     }
     if (row < rows_here) {
       float* P = partial_of(cur.run - first_run) + row * (D + 2);
 #pragma unroll
-      for (int i = 0; i < kCh; i += 2) store_agent(P + c0 + i, acc[i], acc[i + 1]);
-      if (c0 == 0) store_agent(P + D, M, L);
+      for (int i = 0; i < kPairs; ++i) store_agent(P + 32 * i + 2 * n16, acc[i][0], acc[i][1]);
+      if (n16 == 0) store_agent(P + D, M, L);
     }
   }
   if (!arrives_last(a, first_run, live, arrived)) return;
   // groups of 16 threads take (row, every G-th split); few rows leave more groups per row, which are joined through LDS
   int shift = 0;
   while ((1 << shift) < rows_here) ++shift;
-  const int group = tid >> 4, row = group & ((1 << shift) - 1), g0 = group >> shift, G = 16 >> shift, c0 = (tid & 15) * kCh;
-  float M = -INFINITY, L = 0.f, acc[kCh];
+  const int group = tid >> 4, row = group & ((1 << shift) - 1), g0 = group >> shift, G = 16 >> shift, n16 = tid & 15;
+  float M = -INFINITY, L = 0.f;
+  float2v acc[kPairs];
 #pragma unroll
-  for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+  for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
   auto gather = [&](auto ahead) {
     constexpr int kAhead = decltype(ahead)::value;
     for (int s0 = g0; s0 < live; s0 += kAhead * G) {
-      float2v ml[kAhead], x[kAhead][kCh / 2];
+      float2v ml[kAhead], x[kAhead][kPairs];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const float* ps = partial_of(min(s0 + k * G, live - 1)) + row * (D + 2);
         ml[k] = load_agent(ps + D);
 #pragma unroll
-        for (int i = 0; i < kCh / 2; ++i) x[k][i] = load_agent(ps + c0 + 2 * i);
+        for (int i = 0; i < kPairs; ++i) x[k][i] = load_agent(ps + 32 * i + 2 * n16);
       }
       float m2 = M;
 #pragma unroll
@@ -601,13 +600,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       M = m2;
       L *= turn;
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) acc[i] *= turn;
+      for (int i = 0; i < kPairs; ++i) acc[i] *= turn;
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const float e = s0 + k * G < live ? part_factor(ml[k][0], M) : 0.f;
         L = fmaf(e, ml[k][1], L);
 #pragma unroll
-        for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, x[k][i / 2][i & 1], acc[i]);
+        for (int i = 0; i < kPairs; ++i) acc[i] += e * x[k][i];
       }
     }
   };
@@ -615,24 +614,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   if (row < rows_here) live > 2 * G ? gather(std::integral_constant<int, 8>{}) : gather(std::integral_constant<int, 2>{});
   float* flat = &sm_o[0][0][0];
 #pragma unroll
-  for (int i = 0; i < kCh; ++i) flat[group * kStride + c0 + i] = acc[i];
-  float* mls = &sm_m[0][0];  // [group]: M; sm_l: L
-  if (c0 == 0) mls[group] = M, (&sm_l[0][0])[group] = L;
+  for (int i = 0; i < kPairs; ++i) *reinterpret_cast<float2v*>(flat + group * kStride + 32 * i + 2 * n16) = acc[i];
+  float *ms = &sm_m[0][0], *ls = &sm_l[0][0];
+  if (n16 == 0) ms[group] = M, ls[group] = L;
   __syncthreads();
   if (g0 != 0 || row >= rows_here) return;
   float Mt = -INFINITY;
-  for (int k = 0; k < G; ++k) Mt = fmaxf(Mt, mls[(k << shift) + row]);
+  for (int k = 0; k < G; ++k) Mt = fmaxf(Mt, ms[(k << shift) + row]);
   L = 0.f;
 #pragma unroll
-  for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+  for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
   for (int k = 0; k < G; ++k) {
     const int at = (k << shift) + row;
-    const float e = part_factor(mls[at], Mt);
-    L = fmaf(e, (&sm_l[0][0])[at], L);
+    const float e = part_factor(ms[at], Mt);
+    L = fmaf(e, ls[at], L);
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) acc[i] = fmaf(e, flat[at * kStride + c0 + i], acc[i]);
+    for (int i = 0; i < kPairs; ++i) acc[i] += e * *reinterpret_cast<const float2v*>(flat + at * kStride + 32 * i + 2 * n16);
   }
-  write_row<D, BF, kCh>(a, b, h, r0 + row, c0, Mt, L, acc);
+  write_row<D, BF>(a, b, h, r0 + row, n16, Mt, L, acc);
   }();
   __syncthreads();  // the joining has left LDS
   } while (cur.next(a));

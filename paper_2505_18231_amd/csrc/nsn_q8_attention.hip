@@ -1083,14 +1083,16 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   p.tiles = (rows + tile_rows - 1) / tile_rows;
   const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
   const int64_t units = p.tiles * s.n_kv_heads * batch;
-  // runs: two workgroups to each of the 256 compute units (few rows: or one per unit where there are more); four blocks at least (few
-  // rows: a wave each), as a run's start and joining take as long as some blocks
+  // runs: two workgroups to each of the 256 compute units (few rows: or one per unit where there are more).  Where few units reach into
+  // many runs each, one workgroup to a compute unit: it keeps memory nearly as busy and leaves half the partials to be joined (8
+  // units of 2048 blocks 54.6 us and 62.5 us with two, 64 of 32 14.1 and 15.9; 256 of 8 to 256 blocks 116 and 102, 512 of 16 33.2 and
+  // 29.1).  Four blocks at least (few rows: a wave each), as a run's start and joining take as long as some blocks
   const int64_t most = p.chunk ? 512 : kMaxCounters;
   // chunks of many units go one to a workgroup, as joining a cut tile's 128 rows costs about ten of its blocks: with 512 units of 128 to
   // 160 blocks 355 us so and 372 us in equal runs; with ragged chunks of up to 512 units of very different lengths 114 us and 62 us
   p.direct = requested <= 0 && (p.chunk ? units >= (ragged ? 1024 : 512) : units > most);
   p.per = requested > 0 ? 1 : 4;
-  const int64_t runs = requested > 0 ? requested * units : p.chunk ? 512 : std::max<int64_t>(512, units);
+  const int64_t runs = requested > 0 ? requested * units : p.chunk ? 512 : units <= 64 ? 256 : std::max<int64_t>(512, units);
   p.runs = p.direct ? (int)std::min<int64_t>(units, 0x7fffffff)
                     : (int)std::min<int64_t>(std::min<int64_t>(runs, most), (units * blocks + p.per - 1) / p.per);
   // the pass that adds weights up: up to eight workgroups to a compute unit, as sequences may be shorter than max_seq_len and causal

@@ -357,20 +357,21 @@ __device__ __forceinline__ float2v load_agent(const float* p) {
   const unsigned long long u = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return float2v{__uint_as_float((unsigned)u), __uint_as_float((unsigned)(u >> 32))};
 }
-// Counts the workgroup in at a unit that begins in run first_run and reaches into `live`; whether it is the last of them.  (A run
-// is the first of one such unit at most, so its number names the unit's counter.)  The partials are device-scope stores, which no
-// cache holds back; each wave waits until its own are acknowledged, then one thread counts, and the workgroup that counts last
-// reads all partials with device-scope loads.  Nobody waits for anybody else.
-__device__ __forceinline__ bool arrives_last(const Args& a, int first_run, int live, int& arrived) {
+// Counts the workgroup in at a counter that `of` workgroups come to; whether it is the last of them.  The partials are device-scope
+// stores, which no cache holds back; each wave waits until its own are acknowledged, then one thread counts, and the workgroup that
+// counts last reads all partials with device-scope loads.  Nobody waits for anybody else.
+// A run is the first of one unit that goes on behind it at most, and a later one of one other, so run numbers name the counters:
+// kind 0 and 1 by a unit's first run, kind 2 by a later one.
+__device__ __forceinline__ bool arrives_last(const Args& a, int kind, int run, int of, int& arrived) {
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if (threadIdx.x == 0) {
-    int* cnt = a.counters + first_run * kCounterInts;
+    int* cnt = a.counters + (kind * kMaxCounters + run) * kCounterInts;
     arrived = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (arrived == live - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
+    if (arrived == of - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
   }
   __syncthreads();
-  return arrived == live - 1;
+  return arrived == of - 1;
 }
 // factor of a part whose maximum is m in a sum under the maximum M
 __device__ __forceinline__ float part_factor(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
@@ -572,66 +573,87 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       if (n16 == 0) store_agent(P + D, M, L);
     }
   }
-  if (!arrives_last(a, first_run, live, arrived)) return;
-  // groups of 16 threads take (row, every G-th split); few rows leave more groups per row, which are joined through LDS
+  // Partials first, first + step, .. of the unit: all of them where they are few; of a unit that reaches into more than 64 runs,
+  // sixteen at a time, whose sum takes the place of the first, and then those (one head of 71776 tokens: 27.8 us by
+  // one workgroup that reads 225 partials, 17.0 us so).
+  constexpr int kGroup = 16;
+  const bool two = live > 4 * kGroup;
+  const int part = (cur.run - first_run) / kGroup;
+  int from = two ? part * kGroup : 0, n_parts = two ? min(kGroup, live - from) : live, step = 1;
+  if (!arrives_last(a, two ? (part == 0 ? 1 : 2) : 0, first_run + from, n_parts, arrived)) return;
+  // groups of 16 threads take (row, every G-th partial); few rows leave more groups per row, which are joined through LDS
   int shift = 0;
   while ((1 << shift) < rows_here) ++shift;
   const int group = tid >> 4, row = group & ((1 << shift) - 1), g0 = group >> shift, G = 16 >> shift, n16 = tid & 15;
-  float M = -INFINITY, L = 0.f;
-  float2v acc[kPairs];
+  while (true) {
+    float M = -INFINITY, L = 0.f;
+    float2v acc[kPairs];
 #pragma unroll
-  for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
-  auto gather = [&](auto ahead) {
-    constexpr int kAhead = decltype(ahead)::value;
-    for (int s0 = g0; s0 < live; s0 += kAhead * G) {
-      float2v ml[kAhead], x[kAhead][kPairs];
+    for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
+    auto gather = [&](auto ahead) {
+      constexpr int kAhead = decltype(ahead)::value;
+      for (int s0 = g0; s0 < n_parts; s0 += kAhead * G) {
+        float2v ml[kAhead], x[kAhead][kPairs];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const float* ps = partial_of(min(s0 + k * G, live - 1)) + row * (D + 2);
-        ml[k] = load_agent(ps + D);
+        for (int k = 0; k < kAhead; ++k) {
+          const float* ps = partial_of(from + min(s0 + k * G, n_parts - 1) * step) + row * (D + 2);
+          ml[k] = load_agent(ps + D);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) x[k][i] = load_agent(ps + 32 * i + 2 * n16);
+          for (int i = 0; i < kPairs; ++i) x[k][i] = load_agent(ps + 32 * i + 2 * n16);
+        }
+        float m2 = M;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (s0 + k * G < n_parts) m2 = fmaxf(m2, ml[k][0]);
+        const float turn = part_factor(M, m2);
+        M = m2;
+        L *= turn;
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) acc[i] *= turn;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float e = s0 + k * G < n_parts ? part_factor(ml[k][0], M) : 0.f;
+          L = fmaf(e, ml[k][1], L);
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) acc[i] += e * x[k][i];
+        }
       }
-      float m2 = M;
+    };
+    // (a trip to memory takes 2 us, whatever is asked for)
+    if (row < rows_here) n_parts > 2 * G ? gather(std::integral_constant<int, 8>{}) : gather(std::integral_constant<int, 2>{});
+    float* flat = &sm_o[0][0][0];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (s0 + k * G < live) m2 = fmaxf(m2, ml[k][0]);
-      const float turn = part_factor(M, m2);
-      M = m2;
-      L *= turn;
+    for (int i = 0; i < kPairs; ++i) *reinterpret_cast<float2v*>(flat + group * kStride + 32 * i + 2 * n16) = acc[i];
+    float *ms = &sm_m[0][0], *ls = &sm_l[0][0];
+    if (n16 == 0) ms[group] = M, ls[group] = L;
+    __syncthreads();
+    const bool mine = g0 == 0 && row < rows_here;
+    if (mine) {
+      M = -INFINITY, L = 0.f;
+      for (int k = 0; k < G; ++k) M = fmaxf(M, ms[(k << shift) + row]);
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) acc[i] *= turn;
+      for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
+      for (int k = 0; k < G; ++k) {
+        const int at = (k << shift) + row;
+        const float e = part_factor(ms[at], M);
+        L = fmaf(e, ls[at], L);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const float e = s0 + k * G < live ? part_factor(ml[k][0], M) : 0.f;
-        L = fmaf(e, ml[k][1], L);
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) acc[i] += e * x[k][i];
+        for (int i = 0; i < kPairs; ++i) acc[i] += e * *reinterpret_cast<const float2v*>(flat + at * kStride + 32 * i + 2 * n16);
       }
     }
-  };
-  // (a trip to memory takes 2 us, whatever is asked for)
-  if (row < rows_here) live > 2 * G ? gather(std::integral_constant<int, 8>{}) : gather(std::integral_constant<int, 2>{});
-  float* flat = &sm_o[0][0][0];
+    if (!two || step > 1) {
+      if (mine) write_row<D, BF>(a, b, h, r0 + row, n16, M, L, acc);
+      return;
+    }
+    if (mine) {
+      float* P = partial_of(from) + row * (D + 2);
 #pragma unroll
-  for (int i = 0; i < kPairs; ++i) *reinterpret_cast<float2v*>(flat + group * kStride + 32 * i + 2 * n16) = acc[i];
-  float *ms = &sm_m[0][0], *ls = &sm_l[0][0];
-  if (n16 == 0) ms[group] = M, ls[group] = L;
-  __syncthreads();
-  if (g0 != 0 || row >= rows_here) return;
-  float Mt = -INFINITY;
-  for (int k = 0; k < G; ++k) Mt = fmaxf(Mt, ms[(k << shift) + row]);
-  L = 0.f;
-#pragma unroll
-  for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
-  for (int k = 0; k < G; ++k) {
-    const int at = (k << shift) + row;
-    const float e = part_factor(ms[at], Mt);
-    L = fmaf(e, ls[at], L);
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) acc[i] += e * *reinterpret_cast<const float2v*>(flat + at * kStride + 32 * i + 2 * n16);
+      for (int i = 0; i < kPairs; ++i) store_agent(P + 32 * i + 2 * n16, acc[i][0], acc[i][1]);
+      if (n16 == 0) store_agent(P + D, M, L);
+    }
+    from = 0, n_parts = (live + kGroup - 1) / kGroup, step = kGroup;
+    if (!arrives_last(a, 0, first_run, n_parts, arrived)) return;
   }
-  write_row<D, BF>(a, b, h, r0 + row, n16, Mt, L, acc);
   }();
   __syncthreads();  // the joining has left LDS
   } while (cur.next(a));
@@ -828,7 +850,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
         for (int e = 0; e < 16; e += 2) store_agent(P + (8 * i + e / 2) * kThreads * 2, o[i][e] * sref, o[i][e + 1] * sref);
       store_agent(P + kPairs * kThreads * 2, M, l);
     }
-    if (!arrives_last(a, first_run, live, arrived)) return;
+    if (!arrives_last(a, 0, first_run, live, arrived)) return;
     M = -INFINITY, l = 0.f, unit_of_o = 1.f;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
@@ -1025,7 +1047,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void weights_kernel(Args a) {
     const int64_t place = ((int64_t)(b * gridDim.y + h) * (gridDim.x / a.weight_parts) + group) * a.weight_parts;
     float* P = a.partial + place * kWeightTokens + tid;
     __hip_atomic_store(P + part * kWeightTokens, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (!arrives_last(a, (int)(place / a.weight_parts), a.weight_parts, arrived)) return;
+    if (!arrives_last(a, 0, (int)(place / a.weight_parts), a.weight_parts, arrived)) return;
     x = 0.f;
     for (int i = 0; i < a.weight_parts; ++i) x += __hip_atomic_load(P + i * kWeightTokens, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
@@ -1058,8 +1080,14 @@ __global__ __launch_bounds__(kScoreThreads) void weights_of_scores_kernel(Args a
 }
 
 // ---- host side --------------------------------------------------------------------------------------------
-// from this many rows of a (sequence, kv head) on, tiles in LDS
-static bool use_chunk(int64_t rows) { return rows > 32; }
+// Whether rows are taken 128 at a time through tiles in LDS, or 16 at a time.  A tile of 128 rows costs per block three times
+// what one of 16 does, and its joining thirty, so it pays for more than two tiles of 16 where there are enough units to
+// leave most of them whole (128 units of 32 blocks: 32 rows 30.6 us with 128-row tiles and 29.7 without, 48 rows 34 and 40, 128 rows 45
+// and 80; 384 of 5: 48 rows 24.5 and 31), and else from so much work on that the joining does not count (8 units of 128 blocks: 128
+// rows 43 and 23, 512 rows 57 and 58, 1024 rows 69 and 100).
+static bool use_chunk(int64_t rows, int64_t heads, int blocks) {
+  return rows > 32 && ((rows + 32 * kWaves - 1) / (32 * kWaves) * heads >= 128 || (rows + 15) / 16 * heads * blocks >= 28000);
+}
 
 static size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
@@ -1078,10 +1106,10 @@ struct Plan {
 static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int requested, bool weights, bool ragged) {
   Plan p;
   const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads), lines = rows * s.n_kv_heads * batch;
-  p.chunk = use_chunk(rows);
+  const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
+  p.chunk = use_chunk(rows, (int64_t)s.n_kv_heads * batch, blocks);
   const int tile_rows = p.chunk ? 32 * kWaves : 16;
   p.tiles = (rows + tile_rows - 1) / tile_rows;
-  const int blocks = std::max(1, (max_seq_len + kBlock - 1) / kBlock);
   const int64_t units = p.tiles * s.n_kv_heads * batch;
   // runs: two workgroups to each of the 256 compute units (few rows: or one per unit where there are more).  Where few units reach into
   // many runs each, one workgroup to a compute unit: it keeps memory nearly as busy and leaves half the partials to be joined (8
@@ -1091,7 +1119,7 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   // chunks of many units go one to a workgroup, as joining a cut tile's 128 rows costs about ten of its blocks: with 512 units of 128 to
   // 160 blocks 355 us so and 372 us in equal runs; with ragged chunks of up to 512 units of very different lengths 114 us and 62 us
   p.direct = requested <= 0 && (p.chunk ? units >= (ragged ? 1024 : 512) : units > most);
-  p.per = requested > 0 ? 1 : 4;
+  p.per = requested > 0 ? 1 : p.chunk && units < 128 ? 8 : 4;
   const int64_t runs = requested > 0 ? requested * units : p.chunk ? 512 : units <= 64 ? 256 : std::max<int64_t>(512, units);
   p.runs = p.direct ? (int)std::min<int64_t>(units, 0x7fffffff)
                     : (int)std::min<int64_t>(std::min<int64_t>(runs, most), (units * blocks + p.per - 1) / p.per);
@@ -1103,7 +1131,7 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   p.scores = weights && rows <= 16;
   if (weights && p.weight_parts > 1) partials = std::max(partials, (size_t)p.weight_groups * p.weight_parts * kWeightTokens);
   p.score_stride = (int64_t)blocks * kBlock;
-  p.lse2_at = (size_t)kMaxCounters * kCounterInts * sizeof(int);
+  p.lse2_at = (size_t)3 * kMaxCounters * kCounterInts * sizeof(int);
   p.partial_at = p.lse2_at + up16(lines * sizeof(float));
   p.scores_at = p.partial_at + up16(partials * sizeof(float));
   p.bytes = p.scores_at + (p.scores ? (size_t)lines * p.score_stride * sizeof(float) : 0);

@@ -136,6 +136,37 @@ def test_chunks(gpu_api, code, D, io, n_q, ratio, causal):
     run(gpu_api, rng, dev, ratio, lens, n_q, nq=nq, causal=causal, weights=n_q % 2 == 1, strided=True, splits=0 if ratio == 1 else 3)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("code,D,io,page", [(INT8, 128, "fp16", 0), (INT8, 64, "bf16", 128), (E4M3, 128, "bf16", 64), (E4M3, 64, "fp16", 0)])
+@pytest.mark.parametrize("n_q,ratio", [(33, 1), (20, 3), (129, 1), (70, 4)])
+def test_chunks_of_many_heads(gpu_api, code, D, io, page, n_q, ratio, causal):
+    """Enough units that rows go 128 at a time: whole and ragged chunks, longer and shorter than the cache, empty ones, cut into runs."""
+    lens = [0, 1, 64, 130, 384, 300, 65, 256]
+    rng, dev = make(gpu_api, n_q + D, code, D, io, 16, ratio, lens, 384, page)
+    run(gpu_api, rng, dev, ratio, lens, n_q, causal=causal, weights=n_q == 20, strided=n_q == 70)
+    nq = [n_q, 0, n_q - 1, 1, n_q + 5, n_q // 2, n_q, 7]
+    run(gpu_api, rng, dev, ratio, lens, n_q, nq=nq, causal=causal, weights=n_q == 33, splits=3 if n_q > 100 else 0)
+
+
+@pytest.mark.parametrize("code,D", [(INT8, 128), (E4M3, 64)])
+def test_a_long_chunk_of_few_heads(gpu_api, code, D):
+    """So much work that rows go 128 at a time although there are few units: each reaches into many runs."""
+    lens = [14001]
+    rng, dev = make(gpu_api, 3 + D, code, D, "bf16", 1, 1, lens, 14016)
+    run(gpu_api, rng, dev, 1, lens, 2048, nq=[150], causal=True, weights=True)
+    run(gpu_api, rng, dev, 1, lens, 2048, nq=[129])
+
+
+@pytest.mark.parametrize("code,D,io", [(INT8, 128, "fp16"), (E4M3, 64, "bf16")])
+@pytest.mark.parametrize("n_q,ratio", [(1, 1), (1, 5), (3, 7)])
+def test_units_that_reach_into_many_runs(gpu_api, code, D, io, n_q, ratio):
+    """More than 64 runs to a unit: their partial sums are joined in two steps; and just so many."""
+    lens = [6001, 4096, 4097, 70]
+    rng, dev = make(gpu_api, 7 + D, code, D, io, 1, ratio, lens, 6016)
+    for splits in (100, 40, 7):
+        run(gpu_api, rng, dev, ratio, lens, n_q, splits=splits, causal=True, weights=splits == 100)
+
+
 @pytest.mark.parametrize("n_q,causal", [(1, False), (9, True), (150, True), (150, False)])
 @pytest.mark.parametrize("code", [INT8, E4M3])
 def test_pages_that_do_not_exist_hold_no_tokens(gpu_api, code, n_q, causal):
@@ -187,16 +218,16 @@ def test_a_nan_stays_in_its_row(gpu_api):
         assert torch.equal(got, clean)
 
 
-@pytest.mark.parametrize("n_q,lens", [(1, [2000, 700]), (6, [1500, 64]), (200, [900, 333])])
-def test_the_same_call_gives_the_same_bits_and_replays(gpu_api, n_q, lens):
+@pytest.mark.parametrize("n_q,lens,heads", [(1, [2000, 700], 2), (6, [1500, 64], 2), (200, [900, 333], 2), (40, [900, 333], 64)])
+def test_the_same_call_gives_the_same_bits_and_replays(gpu_api, n_q, lens, heads):
     """Twice eagerly, then captured into a graph and replayed between eager calls that share the workspace."""
     import torch
     api = gpu_api
-    rng, dev = make(gpu_api, 31, INT8, 128, "bf16", 2, 4, lens, 2048)
+    rng, dev = make(gpu_api, 31, INT8, 128, "bf16", heads, 4, lens, 2048)
     q, _ = queries(rng, dev, 4, n_q)
     ld = torch.tensor(lens, dtype=torch.int32).cuda()
     ws = torch.zeros(api.nsn_q8_workspace_bytes(dev.shape, api.NSN_OP_Q8_ATTENTION, 2, n_q, 2000), dtype=torch.uint8, device="cuda")
-    w_in = torch.rand((2, 2, 2048), device="cuda")
+    w_in = torch.rand((2, heads, 2048), device="cuda")
 
     def call(out, lse, w):
         api.nsn_q8_attention(dev.shape, q, dev.cache["k"], dev.cache["v"], ld, 2000, 0.09, causal=True, weights_in=w_in, weights_out=w, out=out,
@@ -227,7 +258,7 @@ def test_one_workspace_serves_calls_of_different_sizes_in_turn(gpu_api):
     import torch
     api = gpu_api
     cases = []
-    for seed, D, hkv, ratio, n_q, lens in ((1, 128, 2, 4, 1, [1500, 900]), (2, 64, 5, 1, 1, [777, 3]), (3, 128, 1, 8, 30, [640, 64]), (4, 128, 3, 2, 4, [1111, 1536])):
+    for seed, D, hkv, ratio, n_q, lens in ((1, 128, 2, 4, 1, [1500, 900]), (2, 64, 5, 1, 1, [777, 3]), (3, 128, 1, 8, 30, [640, 64]), (4, 128, 3, 2, 4, [1111, 1536]), (5, 64, 64, 3, 20, [300, 64])):
         rng, dev = make(api, seed, INT8, D, "fp16", hkv, ratio, lens, 1536)
         q, _ = queries(rng, dev, ratio, n_q)
         cases.append((dev, q, torch.tensor(lens, dtype=torch.int32).cuda(), max(lens)))
@@ -315,3 +346,13 @@ def test_a_serving_program_with_a_budget(gpu_api):
             append(a, rng, lens, [1, 1], 1)
             lens = [n + 1 for n in lens]
             attend(1, [1, 1])
+
+
+@pytest.mark.parametrize("code", [INT8, E4M3])
+def test_missing_pages_of_many_heads(gpu_api, code):
+    """The same where rows go 128 at a time."""
+    lens = [512, 300, 130, 511, 64, 0, 400, 200]
+    drop = [(0, 1, -1), (1, 0, 10 ** 9), (1, 2, 40), (2, 0, -7), (2, 1, -2 ** 31), (0, 3, 10), (6, 0, -1), (6, 1, -1), (6, 2, -1), (6, 3, -1)]
+    rng, dev = make(gpu_api, 78, code, 128, "bf16", 16, 2, lens, 512, 128, drop=drop)
+    for causal in (True, False):
+        run(gpu_api, rng, dev, 2, lens, 30, causal=causal, weights=causal)

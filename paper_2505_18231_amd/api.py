@@ -359,7 +359,7 @@ def make_q8_shape(head_dim: int, n_q_heads: int, n_kv_heads: int, max_len: int, 
 
 class Q8Cache:
     """Device buffers of one tensor kind (K or V) in the layout include/nsn.h documents; they stay the same for its lifetime."""
-    __slots__ = ("codes", "scales", "block_table", "c", "device")
+    __slots__ = ("codes", "scales", "block_table", "c", "device", "n_codes", "n_scales", "n_entries")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, block_table: torch.Tensor | None = None):
         assert codes.is_cuda and codes.dtype == torch.uint8 and codes.is_contiguous(), "codes: cuda uint8, contiguous"
@@ -367,6 +367,7 @@ class Q8Cache:
         assert block_table is None or (block_table.dtype == torch.int32 and block_table.is_contiguous() and
                                        block_table.device == codes.device), "block_table: int32, contiguous"
         self.codes, self.scales, self.block_table, self.device = codes, scales, block_table, codes.device
+        self.n_codes, self.n_scales, self.n_entries = codes.numel(), scales.numel(), 0 if block_table is None else block_table.numel()
         self.c = nsn_q8_cache(codes.data_ptr(), scales.data_ptr(), _ptr(block_table))
 
 
@@ -387,26 +388,28 @@ def nsn_q8_workspace_bytes(shape: nsn_q8_shape, op: int, batch: int, n: int, max
     return lib().nsn_q8_workspace_bytes(C.byref(shape), op, batch, n, max_seq_len, n_splits)
 
 
-def _q8_check(shape: nsn_q8_shape, batch: int, *caches: Q8Cache) -> None:
-    device = torch._C._cuda_getDevice()
-    units, tokens = _q8_units(shape, batch)
+def _q8_check(shape: nsn_q8_shape, batch: int, *caches: Q8Cache) -> torch.device:
+    """That the caches hold the shape, on the current device; returns it."""
+    device = caches[0].device
+    assert device.index == torch._C._cuda_getDevice(), "the cache lies on another device than the current one"
+    page, max_len = shape.page_size, shape.max_len
+    heads = (batch * max_len if page <= 0 else shape.n_pages * page) * shape.n_kv_heads
+    n_codes, n_scales = heads * shape.head_dim, heads // 64
     for c in caches:
-        assert c.device.index == device, "the cache lies on another device than the current one"
-        assert c.codes.numel() >= units * shape.n_kv_heads * tokens * shape.head_dim, "codes: too small for the shape"
-        assert c.scales.numel() >= units * shape.n_kv_heads * (tokens // 64), "scales: too small for the shape"
-        if shape.page_size > 0:
-            assert c.block_table is not None and c.block_table.numel() >= batch * (shape.max_len // shape.page_size), \
-                "block_table: [batch][max_len / page_size] needed"
+        assert c.device == device, "the caches lie on different devices"
+        assert c.n_codes >= n_codes and c.n_scales >= n_scales, "codes or scales: too small for the shape"
+        assert page <= 0 or c.n_entries * page >= batch * max_len, "block_table: [batch][max_len / page_size] needed"
+    return device
 
 
 def _q8_small(t: torch.Tensor, device, numel: int, dtype=torch.int32) -> int:
-    assert t.device == device and t.dtype == dtype and t.is_contiguous() and t.numel() >= numel, \
+    assert t.dtype == dtype and t.device == device and t.numel() >= numel and t.is_contiguous(), \
         f"{numel} contiguous values of type {dtype} on {device} needed"
     return t.data_ptr()
 
 
 def _q8_rows(t: torch.Tensor, shape: nsn_q8_shape, device, head: int, token: int) -> nsn_rows:
-    assert t.device == device and t.dtype == shape.dtype, f"rows: {shape.dtype} on {device} needed"
+    assert t.dtype == shape.dtype and t.device == device, f"rows: {shape.dtype} on {device} needed"
     s = t.stride()
     assert s[3] == 1, "rows: the channels of a row must be consecutive"
     return nsn_rows(t.data_ptr(), s[0], s[head], s[token])
@@ -418,8 +421,7 @@ def nsn_q8_append(shape: nsn_q8_shape, k: torch.Tensor, v: torch.Tensor, seq_sta
     [B][max_new][Hkv][D]); seq_start, n_new: cuda int32 [B]."""
     batch, hkv, max_new, d = k.shape
     assert v.shape == k.shape and hkv == shape.n_kv_heads and d == shape.head_dim, "k, v: [batch][n_kv_heads][max_new][head_dim]"
-    _q8_check(shape, batch, k_cache, v_cache)
-    dev = k_cache.device
+    dev = _q8_check(shape, batch, k_cache, v_cache)
     _check(lib().nsn_q8_append(C.byref(shape), C.byref(_q8_rows(k, shape, dev, 1, 2)), C.byref(_q8_rows(v, shape, dev, 1, 2)), max_new,
                                _q8_small(seq_start, dev, batch), _q8_small(n_new, dev, batch), batch, C.byref(k_cache.c),
                                C.byref(v_cache.c), _stream()))
@@ -435,8 +437,7 @@ def nsn_q8_attention(shape: nsn_q8_shape, q: torch.Tensor, k_cache: Q8Cache, v_c
     weights_in, weights_out: fp32 [B][Hkv][max_len].  workspace: zero-filled once (made here if there is none)."""
     batch, n_q, hq, d = q.shape
     assert hq == shape.n_q_heads and d == shape.head_dim, "q: [batch][n_q][n_q_heads][head_dim]"
-    _q8_check(shape, batch, k_cache, v_cache)
-    dev = k_cache.device
+    dev = _q8_check(shape, batch, k_cache, v_cache)
     if out is None:
         out = (torch.empty if q_lens is None else torch.zeros)((batch, n_q, hq, d), dtype=shape.dtype, device=dev)
     if workspace is None:
@@ -462,8 +463,7 @@ def nsn_q8_evict(shape: nsn_q8_shape, weights: torch.Tensor, seq_lens: torch.Ten
     [B][Hkv][max_len]); k_out, v_out are other caches of the same shape (paged: or the same pages under another block table)."""
     batch, hkv = weights.shape[:2]
     assert hkv == shape.n_kv_heads, "weights: [batch][n_kv_heads][max_len]"
-    _q8_check(shape, batch, k_cache, v_cache, k_out, v_out)
-    dev = k_cache.device
+    dev = _q8_check(shape, batch, k_cache, v_cache, k_out, v_out)
     if kept is None:
         kept = torch.empty((batch, hkv, max(keep, 0)), dtype=torch.int32, device=dev)
     if new_lens is None:

@@ -356,3 +356,13 @@ def test_missing_pages_of_many_heads(gpu_api, code):
     rng, dev = make(gpu_api, 78, code, 128, "bf16", 16, 2, lens, 512, 128, drop=drop)
     for causal in (True, False):
         run(gpu_api, rng, dev, 2, lens, 30, causal=causal, weights=causal)
+
+
+@pytest.mark.parametrize("batch,heads,n_q,ratio", [(8, 64, 33, 1), (40, 64, 1, 2), (16, 64, 3, 2), (70, 2, 1, 3), (131, 1, 2, 5), (70, 2, 35, 1), (130, 16, 20, 2)])
+def test_many_sequences_and_heads(gpu_api, batch, heads, n_q, ratio):
+    """More sequences than a wave has lanes, more units than runs, single tokens and chunks; lengths around the blocks, some of zero."""
+    lens = [(37 * i + 5 * (i % 7)) % 140 if i % 11 else 0 for i in range(batch)]
+    rng, dev = make(gpu_api, batch, INT8 if n_q % 2 else E4M3, 64, "fp16", heads, ratio, lens, 192)
+    run(gpu_api, rng, dev, ratio, lens, n_q, causal=n_q > 1)
+    nq = [(i * 7) % (n_q + 1) for i in range(batch)]
+    run(gpu_api, rng, dev, ratio, lens, n_q, nq=nq, weights=heads < 4)

@@ -7,7 +7,7 @@
 //   s = (q . k) * (softmax_scale log2 e sk),  m' = max(m, max s),  p = 2^(s - m'),  l = l 2^(m - m') + sum p,
 //   o = o 2^(m - m') + sv (p . v)
 // Codes become fp16 without loss (int8 and e4m3 both fit), so q . k is exact up to fp32 accumulation; p is rounded to fp16 (half a
-// step 2^-11, below the rounding of the 16-bit output) for the second product.  bf16 queries are multiplied by a power of two
+// step 2^-11, as much as the output where that is fp16) for the second product.  bf16 queries are multiplied by a power of two
 // per row that brings their largest magnitude to 2^14 .. 2^15, and are then fp16 numbers (values 2^-38 below the largest and
 // smaller lose their last bits, which fp32 sums would not keep either).
 #include <algorithm>
@@ -217,17 +217,18 @@ struct Fetched {
 //   - a block's value scale sv enters the exponent, p' = 2^(s - m + kLift + log2(sv / sref)), against a power of two sref that
 //     follows sv when it is off by more than 2^kSpan.  p' stays below 2^(kLift + kLazy + kSpan + 1) <= 2^15, and weights down to 2^-20 of
 //     the row's largest one are normal fp16 numbers.
-// Then sum p v = sref / 2^kLift * (what o holds), sum p = l / 2^kLift with l += (sum p') * (sref / sv).
+// Then sum p v = sref / 2^kLift * (what o holds), sum p = l / 2^kLift with l += (sum p') * (sref / sv).  The output is divided by the sum
+// of the weights as they were rounded (lr), so that a token that holds nearly all of the weight comes out exact; lse goes by l.
 constexpr int kLazy = 4, kSpan = 4, kLift = 6;
 
 // top: the row's largest score of the block; ratio = sref / sv, lift = kLift + log2(sv / sref) for the block
 template <int N, typename V>
-__device__ __forceinline__ void running(float top, float sv, float& m, float& l, float& sref, V (&o)[N], float& ratio, float& lift) {
+__device__ __forceinline__ void running(float top, float sv, float& m, float& l, float& lr, float& sref, V (&o)[N], float& ratio, float& lift) {
   if (__any(top > m + kLazy)) {  // (each row by its own scores: its result does not hang on its neighbours)
     const float m_new = top > m + kLazy ? top : m;
     const float alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
     m = m_new;
-    l *= alpha;
+    l *= alpha, lr *= alpha;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] *= alpha;
   }
@@ -244,6 +245,13 @@ __device__ __forceinline__ void running(float top, float sv, float& m, float& l,
     ratio = sref / sv;
     lift = kLift + __log2f(sv / sref);
   }
+}
+
+// adds a block's weights up: exact and as rounded
+__device__ __forceinline__ float add_rounded(half2v p, float sum) { return __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.f, (_Float16)1.f}, sum, false); }
+__device__ __forceinline__ void add_weights(float sum, float rounded, float ratio, float& l, float& lr) {
+  l = fmaf(sum, ratio, l);
+  lr = fmaf(ratio > 0x1p59f ? sum : rounded, ratio, lr);  // (values so far below the others that the weights underflow: they count all the same)
 }
 
 // ---- the list of the work --------------------------------------------------------------------------------
@@ -376,11 +384,11 @@ __device__ __forceinline__ bool arrives_last(const Args& a, int kind, int run, i
 // factor of a part whose maximum is m in a sum under the maximum M
 __device__ __forceinline__ float part_factor(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
 
-// one row's result: thread n of 16 holds channels 32 i + 2 n, 32 i + 2 n + 1 (acc: sums under the total L)
+// one row's result: thread n of 16 holds channels 32 i + 2 n, 32 i + 2 n + 1 (acc: sums under the total L, R as rounded)
 template <int D, bool BF>
-__device__ __forceinline__ void write_row(const Args& a, int b, int h, int r, int n, float M, float L, const float2v (&acc)[D / 32]) {
+__device__ __forceinline__ void write_row(const Args& a, int b, int h, int r, int n, float M, float L, float R, const float2v (&acc)[D / 32]) {
   const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;
-  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
+  const float inv = R > 0.f ? 1.0f / R : (R == 0.f ? 0.f : R);
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
     *reinterpret_cast<unsigned*>(a.out + place * D + 32 * i + 2 * n) =
@@ -400,7 +408,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   if (!cur.begin(a, blockIdx.x)) return;
   constexpr int kStride = D + 4, kPairs = D / 32;
   __shared__ __attribute__((aligned(16))) float sm_o[kWaves][16][kStride];
-  __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
+  __shared__ float sm_m[kWaves][16], sm_l[kWaves][16], sm_r[kWaves][16];
   __shared__ int arrived;
   do {  // segments
   const int b = cur.b, h = cur.h;
@@ -424,7 +432,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
     x.sk = load_uniform(a.kc.scales + pk), x.sv = load_uniform(a.vc.scales + pv);
   };
   half8v q[D / 32];
-  float factor = 0.f, m = -INFINITY, l = 0.f, sref = 0.f;
+  float factor = 0.f, m = -INFINITY, l = 0.f, lr = 0.f, sref = 0.f;
   float4v o[kCh];
 #pragma unroll
   for (int i = 0; i < kCh; ++i) o[i] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -477,9 +485,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
     top = fmaxf(top, xor_lane<16>(top));
     top = fmaxf(top, xor_lane<32>(top)) * f;
     float ratio, lift;
-    running<kCh>(top, x.sv, m, l, sref, o, ratio, lift);
+    running<kCh>(top, x.sv, m, l, lr, sref, o, ratio, lift);
     const float base = m - lift;
-    float sum = 0.f;
+    float sum = 0.f, rounded = 0.f;
     half8v p[2];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -496,10 +504,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
     for (int j = 0; j < 4; ++j) {
       sum += (s[j][0] + s[j][1]) + (s[j][2] + s[j][3]);
       const half4v u = __builtin_convertvector(s[j], half4v);
+      rounded = add_rounded(half2v{u[2], u[3]}, add_rounded(half2v{u[0], u[1]}, rounded));
 #pragma unroll
       for (int e = 0; e < 4; ++e) p[j >> 1][4 * (j & 1) + e] = u[e];
     }
-    l = fmaf(sum, ratio, l);
+    add_weights(sum, rounded, ratio, l, lr);
 #pragma unroll
     for (int st = 0; st < 2; ++st)
 #pragma unroll
@@ -530,11 +539,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       if (blk >= blk1) break;
     }
   }
-  l += xor_lane<16>(l);
-  l += xor_lane<32>(l);
+  l += xor_lane<16>(l), lr += xor_lane<16>(lr);
+  l += xor_lane<32>(l), lr += xor_lane<32>(lr);
 
   // join the four waves: row n of wave w, channels kCh * (4 kg + e) + i; sums under 2^(m - kLift)
-  if (kg == 0) sm_m[wave][n] = l == 0.f ? -INFINITY : m - kLift, sm_l[wave][n] = l;
+  if (kg == 0) sm_m[wave][n] = l == 0.f ? -INFINITY : m - kLift, sm_l[wave][n] = l, sm_r[wave][n] = lr;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -544,12 +553,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   const int rows_here = min(16, n_rows - r0);
   // the partial of the unit's k-th run: a run has room for two, one of a unit that began before it and one of a unit that
   // begins in it and goes on behind it
-  auto partial_of = [&](int k) { return a.partial + ((int64_t)(first_run + k) * 2 + (k == 0)) * 16 * (D + 2); };
+  auto partial_of = [&](int k) { return a.partial + ((int64_t)(first_run + k) * 2 + (k == 0)) * 16 * (D + 4); };
   [&] {
   {
     // 16 threads per row
     const int row = tid >> 4, n16 = tid & 15;
-    float M = -INFINITY, L = 0.f;
+    float M = -INFINITY, L = 0.f, R = 0.f;
     float2v acc[kPairs];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
@@ -558,19 +567,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float e = part_factor(sm_m[w][row], M);
-      L = fmaf(e, sm_l[w][row], L);
+      L = fmaf(e, sm_l[w][row], L), R = fmaf(e, sm_r[w][row], R);
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) acc[i] += e * *reinterpret_cast<const float2v*>(&sm_o[w][row][32 * i + 2 * n16]);
     }
     if (live == 1) {
-      if (row < rows_here) write_row<D, BF>(a, b, h, r0 + row, n16, M, L, acc);
+      if (row < rows_here) write_row<D, BF>(a, b, h, r0 + row, n16, M, L, R, acc);
       return;
     }
     if (row < rows_here) {
-      float* P = partial_of(cur.run - first_run) + row * (D + 2);
+      float* P = partial_of(cur.run - first_run) + row * (D + 4);
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) store_agent(P + 32 * i + 2 * n16, acc[i][0], acc[i][1]);
-      if (n16 == 0) store_agent(P + D, M, L);
+      if (n16 < 2) store_agent(P + D + 2 * n16, n16 ? R : M, n16 ? 0.f : L);
     }
   }
   // Partials first, first + step, .. of the unit: all of them where they are few; of a unit that reaches into more than 64 runs,
@@ -586,18 +595,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
   while ((1 << shift) < rows_here) ++shift;
   const int group = tid >> 4, row = group & ((1 << shift) - 1), g0 = group >> shift, G = 16 >> shift, n16 = tid & 15;
   while (true) {
-    float M = -INFINITY, L = 0.f;
+    float M = -INFINITY, L = 0.f, R = 0.f;
     float2v acc[kPairs];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
     auto gather = [&](auto ahead) {
       constexpr int kAhead = decltype(ahead)::value;
       for (int s0 = g0; s0 < n_parts; s0 += kAhead * G) {
-        float2v ml[kAhead], x[kAhead][kPairs];
+        float2v ml[kAhead], lr[kAhead], x[kAhead][kPairs];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          const float* ps = partial_of(from + min(s0 + k * G, n_parts - 1) * step) + row * (D + 2);
-          ml[k] = load_agent(ps + D);
+          const float* ps = partial_of(from + min(s0 + k * G, n_parts - 1) * step) + row * (D + 4);
+          ml[k] = load_agent(ps + D), lr[k] = load_agent(ps + D + 2);
 #pragma unroll
           for (int i = 0; i < kPairs; ++i) x[k][i] = load_agent(ps + 32 * i + 2 * n16);
         }
@@ -607,13 +616,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
           if (s0 + k * G < n_parts) m2 = fmaxf(m2, ml[k][0]);
         const float turn = part_factor(M, m2);
         M = m2;
-        L *= turn;
+        L *= turn, R *= turn;
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) acc[i] *= turn;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           const float e = s0 + k * G < n_parts ? part_factor(ml[k][0], M) : 0.f;
-          L = fmaf(e, ml[k][1], L);
+          L = fmaf(e, ml[k][1], L), R = fmaf(e, lr[k][0], R);
 #pragma unroll
           for (int i = 0; i < kPairs; ++i) acc[i] += e * x[k][i];
         }
@@ -624,32 +633,32 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
     float* flat = &sm_o[0][0][0];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) *reinterpret_cast<float2v*>(flat + group * kStride + 32 * i + 2 * n16) = acc[i];
-    float *ms = &sm_m[0][0], *ls = &sm_l[0][0];
-    if (n16 == 0) ms[group] = M, ls[group] = L;
+    float *ms = &sm_m[0][0], *ls = &sm_l[0][0], *rs = &sm_r[0][0];
+    if (n16 == 0) ms[group] = M, ls[group] = L, rs[group] = R;
     __syncthreads();
     const bool mine = g0 == 0 && row < rows_here;
     if (mine) {
-      M = -INFINITY, L = 0.f;
+      M = -INFINITY, L = R = 0.f;
       for (int k = 0; k < G; ++k) M = fmaxf(M, ms[(k << shift) + row]);
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) acc[i] = float2v{0.f, 0.f};
       for (int k = 0; k < G; ++k) {
         const int at = (k << shift) + row;
         const float e = part_factor(ms[at], M);
-        L = fmaf(e, ls[at], L);
+        L = fmaf(e, ls[at], L), R = fmaf(e, rs[at], R);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) acc[i] += e * *reinterpret_cast<const float2v*>(flat + at * kStride + 32 * i + 2 * n16);
       }
     }
     if (!two || step > 1) {
-      if (mine) write_row<D, BF>(a, b, h, r0 + row, n16, M, L, acc);
+      if (mine) write_row<D, BF>(a, b, h, r0 + row, n16, M, L, R, acc);
       return;
     }
     if (mine) {
-      float* P = partial_of(from) + row * (D + 2);
+      float* P = partial_of(from) + row * (D + 4);
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) store_agent(P + 32 * i + 2 * n16, acc[i][0], acc[i][1]);
-      if (n16 == 0) store_agent(P + D, M, L);
+      if (n16 < 2) store_agent(P + D + 2 * n16, n16 ? R : M, n16 ? 0.f : L);
     }
     from = 0, n_parts = (live + kGroup - 1) / kGroup, step = kGroup;
     if (!arrives_last(a, 0, first_run, n_parts, arrived)) return;
@@ -696,7 +705,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
 
   half8v q[D / 16];
   const float factor = load_query_rows<D, BF>(a, b, h, r, pr.nq, q);
-  float m = -INFINITY, l = 0.f, sref = 0.f;
+  float m = -INFINITY, l = 0.f, lr = 0.f, sref = 0.f;
   float16v o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
@@ -802,9 +811,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[j][e]);
       top = fmaxf(top, xor_lane<32>(top)) * f;
       float ratio, lift;
-      running<D / 32>(top, sv, m, l, sref, o, ratio, lift);
+      running<D / 32>(top, sv, m, l, lr, sref, o, ratio, lift);
       const float base = m - lift;
-      float sum[2] = {0.f, 0.f};
+      float sum[2] = {0.f, 0.f}, rounded[2] = {0.f, 0.f};
       half8v p[4];
 #pragma unroll
       for (int j = 0; j < 2; ++j)
@@ -823,9 +832,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
         for (int e = 0; e < 16; e += 2) {
           sum[0] += s[j][e], sum[1] += s[j][e + 1];
           const half2v u = __builtin_convertvector((float2v{s[j][e], s[j][e + 1]}), half2v);
+          rounded[j] = add_rounded(u, rounded[j]);
           p[2 * j + e / 8][e % 8] = u[0], p[2 * j + e / 8][e % 8 + 1] = u[1];
         }
-      l = fmaf(sum[0] + sum[1], ratio, l);
+      add_weights(sum[0] + sum[1], rounded[0] + rounded[1], ratio, l, lr);
 #pragma unroll
       for (int st = 0; st < 4; ++st)
 #pragma unroll
@@ -834,14 +844,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     }
     if (blk + 1 < blk1 && next_there) stage(sm[buf ^ 1]);
   }
-  l += xor_lane<32>(l);
+  l += xor_lane<32>(l), lr += xor_lane<32>(lr);
   // o[i][e]: row 32 i + 8 (e / 4) + 4 hh + e % 4 of the transposed values; the channels of cell c are its rows 16 x + c
   float M = l == 0.f ? -INFINITY : m - kLift, unit_of_o = sref;
   [&] {
   if (live > 1) {
     // the sums as they lie in the threads, two to a store; joined in the order of the runs
     constexpr int kPairs = D / 4, kThreads = kWaves * 64;
-    auto partial_of = [&](int k) { return a.partial + (((int64_t)(first_run + k) * 2 + (k == 0)) * (kPairs + 1) * kThreads + tid) * 2; };
+    auto partial_of = [&](int k) { return a.partial + (((int64_t)(first_run + k) * 2 + (k == 0)) * (kPairs + 2) * kThreads + tid) * 2; };
     float* P = partial_of(cur.run - first_run);
     if (r < n_rows) {
 #pragma unroll
@@ -849,9 +859,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
 #pragma unroll
         for (int e = 0; e < 16; e += 2) store_agent(P + (8 * i + e / 2) * kThreads * 2, o[i][e] * sref, o[i][e + 1] * sref);
       store_agent(P + kPairs * kThreads * 2, M, l);
+      store_agent(P + (kPairs + 1) * kThreads * 2, lr, 0.f);
     }
     if (!arrives_last(a, 0, first_run, live, arrived)) return;
-    M = -INFINITY, l = 0.f, unit_of_o = 1.f;
+    M = -INFINITY, l = lr = 0.f, unit_of_o = 1.f;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -859,13 +870,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     if (r < n_rows)
       for (int k = 0; k < live; ++k) {
         const float* ps = partial_of(k);
-        const float2v ml = load_agent(ps + kPairs * kThreads * 2);
+        const float2v ml = load_agent(ps + kPairs * kThreads * 2), rd = load_agent(ps + (kPairs + 1) * kThreads * 2);
         float2v x[kPairs];
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) x[i] = load_agent(ps + i * kThreads * 2);
         const float m2 = fmaxf(M, ml[0]), turn = part_factor(M, m2), f = part_factor(ml[0], m2);
         M = m2;
-        l = fmaf(f, ml[1], l * turn);
+        l = fmaf(f, ml[1], l * turn), lr = fmaf(f, rd[0], lr * turn);
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -874,7 +885,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
   }
   if (r >= n_rows) return;
   const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;
-  const float inv = l > 0.f ? unit_of_o / l : (l == 0.f ? 0.f : l);
+  const float inv = lr > 0.f ? unit_of_o / lr : (lr == 0.f ? 0.f : lr);
 #pragma unroll
   for (int c4 = 0; c4 < 2; ++c4)
 #pragma unroll
@@ -1114,12 +1125,13 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   // runs: two workgroups to each of the 256 compute units (few rows: or one per unit where there are more).  Where few units reach into
   // many runs each, one workgroup to a compute unit: it keeps memory nearly as busy and leaves half the partials to be joined (8
   // units of 2048 blocks 54.6 us and 62.5 us with two, 64 of 32 14.1 and 15.9; 256 of 8 to 256 blocks 116 and 102, 512 of 16 33.2 and
-  // 29.1).  Four blocks at least (few rows: a wave each), as a run's start and joining take as long as some blocks
+  // 29.1).  Four blocks at least (few rows: a wave each; chunks of few units eight), as a run's start and joining take as long as some
+  // blocks, but no more than a unit has: units one after the other cost their trips to memory one after the other
   const int64_t most = p.chunk ? 512 : kMaxCounters;
   // chunks of many units go one to a workgroup, as joining a cut tile's 128 rows costs about ten of its blocks: with 512 units of 128 to
   // 160 blocks 355 us so and 372 us in equal runs; with ragged chunks of up to 512 units of very different lengths 114 us and 62 us
   p.direct = requested <= 0 && (p.chunk ? units >= (ragged ? 1024 : 512) : units > most);
-  p.per = requested > 0 ? 1 : p.chunk && units < 128 ? 8 : 4;
+  p.per = requested > 0 ? 1 : std::min(p.chunk && units < 128 ? 8 : 4, blocks);
   const int64_t runs = requested > 0 ? requested * units : p.chunk ? 512 : units <= 64 ? 256 : std::max<int64_t>(512, units);
   p.runs = p.direct ? (int)std::min<int64_t>(units, 0x7fffffff)
                     : (int)std::min<int64_t>(std::min<int64_t>(runs, most), (units * blocks + p.per - 1) / p.per);
@@ -1127,7 +1139,7 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   // parts unequal, each with four tiles of rows at least; its partial sums come after the attention's and take their place
   p.weight_groups = (blocks + kWaves - 1) / kWaves * (int64_t)s.n_kv_heads * batch;
   p.weight_parts = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCounters / p.weight_groups, rows / (4 * kWeightRows)));
-  size_t partials = p.direct ? 0 : (size_t)p.runs * 2 * (p.chunk ? (s.head_dim / 2 + 2) * kWaves * 64 : 16 * (s.head_dim + 2));
+  size_t partials = p.direct ? 0 : (size_t)p.runs * 2 * (p.chunk ? (s.head_dim / 2 + 4) * kWaves * 64 : 16 * (s.head_dim + 4));
   p.scores = weights && rows <= 16;
   if (weights && p.weight_parts > 1) partials = std::max(partials, (size_t)p.weight_groups * p.weight_parts * kWeightTokens);
   p.score_stride = (int64_t)blocks * kBlock;

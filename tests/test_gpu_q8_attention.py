@@ -4,8 +4,9 @@ Tolerances, from the roundings (u16 = half a step of the output's type: 2^-11 fp
   score   the products are exact in fp32 (fp16 x 8-bit), their sum over D channels is off by at most D 2^-24 sum|q k|; two more
           roundings, and the softmax scale's, each 2^-24 of the score itself (which sum|q k| bounds).  With e = scale (D + 8) 2^-24
           max_t sum|q_c k_c| the relative error of a weight p is 2 e + 2^-20 (its own score, the row's sum; exponential and sums).
-  out     |o - o'| <= (2^-11 + 2 e + 2^-19) sum p|v| + 2^-24 sum_t |v_t| + u16 |o|: weights rounded to fp16 (2^-11 relative, 2^-25
-          absolute where they are subnormal next to the row's largest weight), then the output's rounding
+  out     |o - o'| <= (2^-11 + 2 e + 2^-19) (sum p|v| + |o|) + 2^-24 sum_t |v_t| + u16 |o|: weights rounded to fp16 (2^-11 relative,
+          2^-25 absolute where they are subnormal next to the row's largest weight) and divided by their own sum: with relative errors
+          d_t, o' - o = sum p d_t (v_t - o) / (1 + sum p d_t), and |v_t - o| <= |v_t| + |o|; then the output's rounding
   lse     e + 2^-21 (1 + |lse|)
   weights sum of p (2 e + 2^-20) over the rows + 2^-23 |the result|
 """
@@ -59,7 +60,7 @@ def compare(dev, ref_q, out, lse, lens, nq, scale, causal, ratio, out0, lse0, we
                 seen = (np.arange(n)[None, :] < vis[:, None]) & exists[None, :]
                 o, z, p, pv = R.attention(q, k, v, scale, seen)
                 e = abs(scale) * (D + 8) * 2.0 ** -24 * np.where(seen, np.abs(q) @ np.abs(k).T, 0).max(axis=1, initial=0.0)
-                tol = (2.0 ** -11 + 2 * e[:, None] + 2.0 ** -19) * pv + 2.0 ** -24 * (seen @ np.abs(v)) + u16 * np.abs(o)
+                tol = (2.0 ** -11 + 2 * e[:, None] + 2.0 ** -19) * (pv + np.abs(o)) + 2.0 ** -24 * (seen @ np.abs(v)) + u16 * np.abs(o)
                 tol = tol * (1 + u16) + 2.0 ** -25      # (the output's rounding of what is already off; its subnormal step)
                 d = np.abs(out[b, :m, hq] - o)
                 assert (d <= tol).all(), (b, h, g, float((d / tol).max()))

@@ -366,7 +366,7 @@ class Q8Cache:
         assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.device == codes.device, "scales: fp32, contiguous"
         assert block_table is None or (block_table.dtype == torch.int32 and block_table.is_contiguous() and
                                        block_table.device == codes.device), "block_table: int32, contiguous"
-        self.codes, self.scales, self.block_table, self.device = codes, scales, block_table, codes.device
+        self.codes, self.scales, self.block_table, self.device = codes, scales, block_table, codes.get_device()
         self.n_codes, self.n_scales, self.n_entries = codes.numel(), scales.numel(), 0 if block_table is None else block_table.numel()
         self.c = nsn_q8_cache(codes.data_ptr(), scales.data_ptr(), _ptr(block_table))
 
@@ -388,29 +388,28 @@ def nsn_q8_workspace_bytes(shape: nsn_q8_shape, op: int, batch: int, n: int, max
     return lib().nsn_q8_workspace_bytes(C.byref(shape), op, batch, n, max_seq_len, n_splits)
 
 
-def _q8_check(shape: nsn_q8_shape, batch: int, *caches: Q8Cache) -> torch.device:
-    """That the caches hold the shape, on the current device; returns it."""
-    device = caches[0].device
-    assert device.index == torch._C._cuda_getDevice(), "the cache lies on another device than the current one"
+def _q8_check(shape: nsn_q8_shape, batch: int, *caches: Q8Cache) -> int:
+    """That the caches hold the shape, on the current device; returns its index."""
+    device = torch._C._cuda_getDevice()
     page, max_len = shape.page_size, shape.max_len
     heads = (batch * max_len if page <= 0 else shape.n_pages * page) * shape.n_kv_heads
     n_codes, n_scales = heads * shape.head_dim, heads // 64
     for c in caches:
-        assert c.device == device, "the caches lie on different devices"
+        assert c.device == device, "the cache lies on another device than the current one"
         assert c.n_codes >= n_codes and c.n_scales >= n_scales, "codes or scales: too small for the shape"
         assert page <= 0 or c.n_entries * page >= batch * max_len, "block_table: [batch][max_len / page_size] needed"
     return device
 
 
-def _q8_small(t: torch.Tensor, device, numel: int, dtype=torch.int32) -> int:
-    assert t.dtype == dtype and t.device == device and t.numel() >= numel and t.is_contiguous(), \
-        f"{numel} contiguous values of type {dtype} on {device} needed"
+def _q8_small(t: torch.Tensor, device: int, numel: int, dtype=torch.int32) -> int:
+    assert t.dtype is dtype and t.get_device() == device and t.numel() >= numel and t.is_contiguous(), \
+        f"{numel} contiguous values of type {dtype} on device {device} needed"
     return t.data_ptr()
 
 
-def _q8_rows(t: torch.Tensor, shape: nsn_q8_shape, device, head: int, token: int) -> nsn_rows:
-    assert t.dtype == shape.dtype and t.device == device, f"rows: {shape.dtype} on {device} needed"
+def _q8_rows(t: torch.Tensor, shape: nsn_q8_shape, device: int, head: int, token: int) -> nsn_rows:
     s = t.stride()
+    assert t.dtype is shape.dtype and t.get_device() == device, f"rows: {shape.dtype} on device {device} needed"
     assert s[3] == 1, "rows: the channels of a row must be consecutive"
     return nsn_rows(t.data_ptr(), s[0], s[head], s[token])
 
@@ -424,7 +423,7 @@ def nsn_q8_append(shape: nsn_q8_shape, k: torch.Tensor, v: torch.Tensor, seq_sta
     dev = _q8_check(shape, batch, k_cache, v_cache)
     _check(lib().nsn_q8_append(C.byref(shape), C.byref(_q8_rows(k, shape, dev, 1, 2)), C.byref(_q8_rows(v, shape, dev, 1, 2)), max_new,
                                _q8_small(seq_start, dev, batch), _q8_small(n_new, dev, batch), batch, C.byref(k_cache.c),
-                               C.byref(v_cache.c), _stream()))
+                               C.byref(v_cache.c), torch._C._cuda_getCurrentRawStream(dev)))
 
 
 def nsn_q8_attention(shape: nsn_q8_shape, q: torch.Tensor, k_cache: Q8Cache, v_cache: Q8Cache, seq_lens: torch.Tensor,
@@ -443,15 +442,20 @@ def nsn_q8_attention(shape: nsn_q8_shape, q: torch.Tensor, k_cache: Q8Cache, v_c
     if workspace is None:
         need = nsn_q8_workspace_bytes(shape, NSN_OP_Q8_ATTENTION, batch, n_q, max_seq_len, n_splits)
         workspace = torch.zeros(max(need, 1), dtype=torch.uint8, device=dev)
-    n_w = batch * shape.n_kv_heads * shape.max_len
+    w_in = w_out = None
+    if weights_out is not None:
+        n_w = batch * shape.n_kv_heads * shape.max_len
+        w_out = _q8_small(weights_out, dev, n_w, torch.float32)
+        w_in = None if weights_in is None else _q8_small(weights_in, dev, n_w, torch.float32)
+    else:
+        assert weights_in is None, "weights_in without weights_out"
     _check(lib().nsn_q8_attention(C.byref(shape), C.byref(_q8_rows(q, shape, dev, 2, 1)), n_q,
                                   None if q_lens is None else _q8_small(q_lens, dev, batch), C.byref(k_cache.c), C.byref(v_cache.c),
-                                  _q8_small(seq_lens, dev, batch), batch, max_seq_len, float(softmax_scale), int(causal),
-                                  None if weights_in is None else _q8_small(weights_in, dev, n_w, torch.float32),
-                                  None if weights_out is None else _q8_small(weights_out, dev, n_w, torch.float32), n_splits,
+                                  _q8_small(seq_lens, dev, batch), batch, max_seq_len, softmax_scale, causal, w_in, w_out, n_splits,
                                   _q8_small(out, dev, q.numel(), shape.dtype),
                                   None if lse is None else _q8_small(lse, dev, batch * n_q * hq, torch.float32),
-                                  _q8_small(workspace, dev, 0, torch.uint8), workspace.numel(), _stream()))
+                                  _q8_small(workspace, dev, 0, torch.uint8), workspace.numel(),
+                                  torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 

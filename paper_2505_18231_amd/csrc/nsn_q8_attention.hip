@@ -242,8 +242,10 @@ __device__ __forceinline__ void running(float top, float sv, float& m, float& l,
 #pragma unroll
       for (int i = 0; i < N; ++i) o[i] *= turn;
     }
-    ratio = sref / sv;
-    lift = kLift + __log2f(sv / sref);
+    // (sref is a power of two, and sv / sref a normal number: the instructions themselves will do, half a dozen of them for two dozen)
+    const float inv_sv = __builtin_amdgcn_rcpf(sv);
+    ratio = sref * inv_sv;
+    lift = kLift - __builtin_amdgcn_logf(ratio);
   }
 }
 

@@ -368,13 +368,13 @@ enum { NSN_FP16 = 0, NSN_BF16 = 1 };
 
 typedef struct nsn_q8_shape {
   int32_t head_dim;   /* 64 or 128 */
-  int32_t n_q_heads;  /* a multiple of n_kv_heads */
-  int32_t n_kv_heads;
+  int32_t n_q_heads;  /* a multiple of n_kv_heads, at most 65535 */
+  int32_t n_kv_heads; /* at most 32767 */
   int32_t code_type;  /* NSN_Q8_INT8 or NSN_Q8_E4M3 */
   int32_t io_type;    /* NSN_FP16 or NSN_BF16: type of the new rows, the queries and the output */
   int32_t page_size;  /* 0 = contiguous; else tokens per page, multiple of 64 */
   int32_t n_pages;    /* paged: physical pages of the cache */
-  int32_t max_len;    /* token capacity per sequence, multiple of 64 (and of page_size) */
+  int32_t max_len;    /* token capacity per sequence, multiple of 64 (and of page_size), at most 2^30 */
 } nsn_q8_shape;
 
 typedef struct nsn_q8_cache {
@@ -397,9 +397,9 @@ int64_t nsn_q8_v_code_offset(const nsn_q8_shape* shape, int64_t t, int c);
  * Device bytes an operation needs, for sequences of up to max_seq_len tokens.
  *   NSN_OP_Q8_ATTENTION  n = n_q; n_splits as passed to nsn_q8_attention (0 = auto).  Fill the workspace with zeros
  *                        ONCE after allocating it; every call leaves it ready for the next one, of any size.
- *   NSN_OP_Q8_EVICT      n = keep; n_splits ignored.  Needs no preparation.
- * It starts on a 16-byte boundary.  Calls that share a workspace must not overlap in time, and the two operations do not
- * share one.  Returns 0 for an invalid shape or size.
+ *   NSN_OP_Q8_EVICT      needs none: 0
+ * It starts on a 16-byte boundary.  Calls that share a workspace must not overlap in time.  Returns 0 for an invalid shape or
+ * size.
  */
 size_t nsn_q8_workspace_bytes(const nsn_q8_shape* shape, int op, int batch, int n, int max_seq_len, int n_splits);
 
@@ -411,6 +411,8 @@ size_t nsn_q8_workspace_bytes(const nsn_q8_shape* shape, int op, int batch, int 
  *   k, v          rows by (sequence, kv head, token), at least max_new tokens each; rows >= n_new[b] are not read
  *   seq_start, n_new  dev int32 [batch].  n_new is taken as at most max_new; a negative start or count writes nothing;
  *                 tokens beyond max_len are not written
+ *   k_cache, v_cache  share no memory.  Paged: a 64-token block that a call writes belongs to one sequence (pages that
+ *                 several sequences name are read by all of them, but written through none)
  * Errors: INVALID_ARG, UNSUPPORTED, HIP.
  */
 int nsn_q8_append(const nsn_q8_shape* shape, const nsn_rows* k, const nsn_rows* v, int max_new,
@@ -432,11 +434,15 @@ int nsn_q8_append(const nsn_q8_shape* shape, const nsn_rows* k, const nsn_rows* 
  *   weights_in, weights_out  fp32 [batch][n_kv_heads][max_len], or NULL.  With weights_out,
  *                 weights_out[b][h][t] = weights_in[b][h][t] + sum over the queries i < q_lens[b] and the query heads
  *                 of kv head h of softmax(score_i)_t,  for t < seq_lens[b]; the rest of weights_out is not written.
- *                 weights_in may be weights_out, or NULL (zeros).
- *   n_splits      partitions of the token axis that are worked on at the same time and merged (0 = choose)
- *   out           io_type [batch][n_q][n_q_heads][head_dim], 16-byte aligned
+ *                 weights_in may be weights_out, or NULL (zeros), but may not overlap it otherwise.  A call with n_q = 0
+ *                 adds nothing: there weights_in must be weights_out.
+ *   n_splits      by how many workgroups the tokens of a tile of rows are worked on at the same time, as far as there are
+ *                 as many blocks of 64 and 2048 workgroups suffice (0 = choose).  Results differ by fp32 rounding only
+ *   out           io_type [batch][n_q][n_q_heads][head_dim], 16-byte aligned; not between the first and the last row of q
  *   lse           fp32 [batch][n_q][n_q_heads], or NULL
- * Scores, sums and the output are accumulated in fp32; the weights p enter the second product as fp16.
+ * Scores, sums and the output are accumulated in fp32; the weights p enter the second product as fp16, and the output is
+ * divided by their sum as rounded (lse: by the sum before rounding).  The same call gives the same bits, whatever else runs; a
+ * sequence's last bits may depend on the other sequences' lengths, which decide where its tokens are cut.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
  */
 int nsn_q8_attention(const nsn_q8_shape* shape, const nsn_rows* q, int n_q, const int32_t* q_lens_dev,
@@ -453,13 +459,15 @@ int nsn_q8_attention(const nsn_q8_shape* shape, const nsn_rows* q, int n_q, cons
  * nearest even.
  *   weights      fp32 [batch][n_kv_heads][max_len] (weights_out of nsn_q8_attention), 16-byte aligned
  *   k_cache, v_cache  the caches read; k_out, v_out those written, of the same shape: other buffers, or (paged) the same
- *                ones under a block table that shares no page with what is read
+ *                ones under a block table that shares no page with what is read.  A page that does not exist among those read
+ *                gives zeros
  *   first, recent  >= 0, first + recent <= keep;  1 <= keep <= max_len
  *   kept         out, int32 [batch][n_kv_heads][keep]: former indices, ascending; -1 behind the last
- *   new_lens     out, int32 [batch] = min(seq_lens[b], keep)
+ *   new_lens     out, int32 [batch] = min(seq_lens[b], keep); not the buffer seq_lens
  *   weights_out  out, fp32 [batch][n_kv_heads][max_len], or NULL: the kept tokens' weights, then zeros up to max_seq_len
- *                (not the buffer `weights`)
- * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ *                (not in the buffer `weights`)
+ *   workspace    not used: may be NULL with workspace_bytes = 0
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
  */
 int nsn_q8_evict(const nsn_q8_shape* shape, const float* weights, const int32_t* seq_lens_dev, int batch,
                  int max_seq_len, int keep, int first, int recent, const nsn_q8_cache* k_cache,

@@ -384,7 +384,7 @@ def alloc_q8_cache(shape: nsn_q8_shape, batch: int, device="cuda", block_table: 
 
 
 def nsn_q8_workspace_bytes(shape: nsn_q8_shape, op: int, batch: int, n: int, max_seq_len: int, n_splits: int = 0) -> int:
-    """op: NSN_OP_Q8_ATTENTION (n = n_q) or NSN_OP_Q8_EVICT (n = keep)."""
+    """op: NSN_OP_Q8_ATTENTION (n = n_q); NSN_OP_Q8_EVICT needs none (0)."""
     return lib().nsn_q8_workspace_bytes(C.byref(shape), op, batch, n, max_seq_len, n_splits)
 
 
@@ -464,7 +464,8 @@ def nsn_q8_evict(shape: nsn_q8_shape, weights: torch.Tensor, seq_lens: torch.Ten
                  kept: torch.Tensor | None = None, new_lens: torch.Tensor | None = None, weights_out: torch.Tensor | None = None,
                  workspace: torch.Tensor | None = None):
     """weights: cuda fp32 [B][Hkv][max_len].  Returns (kept int32 [B][Hkv][keep], new_lens int32 [B], weights_out fp32
-    [B][Hkv][max_len]); k_out, v_out are other caches of the same shape (paged: or the same pages under another block table)."""
+    [B][Hkv][max_len]); k_out, v_out are other caches of the same shape (paged: or the same pages under another block table).
+    workspace: not used."""
     batch, hkv = weights.shape[:2]
     assert hkv == shape.n_kv_heads, "weights: [batch][n_kv_heads][max_len]"
     dev = _q8_check(shape, batch, k_cache, v_cache, k_out, v_out)
@@ -474,13 +475,10 @@ def nsn_q8_evict(shape: nsn_q8_shape, weights: torch.Tensor, seq_lens: torch.Ten
         new_lens = torch.empty(batch, dtype=torch.int32, device=dev)
     if weights_out is None:
         weights_out = torch.zeros_like(weights)
-    if workspace is None:
-        need = nsn_q8_workspace_bytes(shape, NSN_OP_Q8_EVICT, batch, keep, max_seq_len)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
     n_w = batch * hkv * shape.max_len
     _check(lib().nsn_q8_evict(C.byref(shape), _q8_small(weights, dev, n_w, torch.float32), _q8_small(seq_lens, dev, batch), batch,
                               max_seq_len, keep, first, recent, C.byref(k_cache.c), C.byref(v_cache.c), C.byref(k_out.c),
                               C.byref(v_out.c), _q8_small(kept, dev, batch * hkv * keep), _q8_small(new_lens, dev, batch),
-                              _q8_small(weights_out, dev, n_w, torch.float32), _q8_small(workspace, dev, 0, torch.uint8),
-                              workspace.numel(), _stream()))
+                              _q8_small(weights_out, dev, n_w, torch.float32), _ptr(workspace),
+                              0 if workspace is None else workspace.numel(), _stream()))
     return kept, new_lens, weights_out

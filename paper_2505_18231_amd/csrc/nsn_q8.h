@@ -202,10 +202,8 @@ struct EvictCall {
   nsn_q8_cache kc, vc, ko, vo;
   int32_t *kept, *new_lens;
   float* weights_out;
-  void* workspace;
   hipStream_t stream;
 };
-size_t evict_workspace_bytes(const nsn_q8_shape& s, int batch, int keep, int max_seq_len);
 int evict_launch(const EvictCall& c);
 
 // calls f with integral constants (head_dim, code type, BF16 rows)

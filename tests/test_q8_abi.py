@@ -10,6 +10,7 @@ from paper_2505_18231_amd import api
 from tests import q8_reference as R
 
 FAKE = 0x10000   # an aligned address that no call may reach
+FAR = 1 << 44
 
 
 @pytest.fixture(scope="module")
@@ -52,26 +53,25 @@ def test_offsets_are_the_header_s_and_a_bijection(L, D):
 BAD_SHAPES = [(dict(head_dim=96), -2), (dict(code_type=2), -2), (dict(io_type=2), -2), (dict(io_type=-1), -2), (dict(n_q_heads=12), -1),
               (dict(n_kv_heads=0), -1), (dict(n_q_heads=0), -1), (dict(n_q_heads=65536, n_kv_heads=1), -1), (dict(max_len=100), -1),
               (dict(max_len=0), -1), (dict(page_size=48), -1), (dict(page_size=-64), -1), (dict(page_size=192, n_pages=5), -1),
-              (dict(page_size=64, n_pages=0), -1)]
+              (dict(page_size=64, n_pages=0), -1), (dict(n_q_heads=32768, n_kv_heads=32768), -1), (dict(max_len=(1 << 30) + 64), -1)]
 
 
 def append(L, s, k=None, v=None, max_new=4, start=FAKE, n=FAKE, batch=1, kc=None, vc=None):
     return L.nsn_q8_append(C.byref(s), C.byref(k or rows()), C.byref(v or rows()), max_new, start, n, batch,
-                           C.byref(kc or cache()), C.byref(vc or cache()), None)
+                           C.byref(kc or cache()), C.byref(vc or cache(codes=FAR, scales=FAR)), None)
 
 
 def attend(L, s, q=None, n_q=1, q_lens=None, kc=None, vc=None, lens=FAKE, batch=1, max_seq=1024, scale=1.0, w_in=None, w_out=None,
-           splits=0, out=FAKE, lse=None, ws=FAKE, ws_bytes=1 << 40):
+           splits=0, out=FAR, lse=None, ws=FAKE, ws_bytes=1 << 40):
     return L.nsn_q8_attention(C.byref(s), C.byref(q or rows()), n_q, q_lens, C.byref(kc or cache()), C.byref(vc or cache()), lens, batch,
                               max_seq, scale, 0, w_in, w_out, splits, out, lse, ws, ws_bytes, None)
 
 
 def evict(L, s, w=FAKE, lens=FAKE, batch=1, max_seq=1024, keep=64, first=0, recent=0, kc=None, vc=None, ko=None, vo=None, kept=FAKE,
-          new=FAKE, w_out=None, ws=FAKE, ws_bytes=1 << 40):
-    far = 1 << 44
-    return L.nsn_q8_evict(C.byref(s), w, lens, batch, max_seq, keep, first, recent, C.byref(kc or cache(codes=far, scales=far)),
-                          C.byref(vc or cache(codes=2 * far, scales=2 * far)), C.byref(ko or cache(codes=3 * far, scales=3 * far)),
-                          C.byref(vo or cache(codes=4 * far, scales=4 * far)), kept, new, w_out, ws, ws_bytes, None)
+          new=FAR, w_out=None, ws=FAKE, ws_bytes=1 << 40):
+    return L.nsn_q8_evict(C.byref(s), w, lens, batch, max_seq, keep, first, recent, C.byref(kc or cache(codes=FAR, scales=FAR)),
+                          C.byref(vc or cache(codes=2 * FAR, scales=2 * FAR)), C.byref(ko or cache(codes=3 * FAR, scales=3 * FAR)),
+                          C.byref(vo or cache(codes=4 * FAR, scales=4 * FAR)), kept, new, w_out, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw,rc", BAD_SHAPES)
@@ -109,7 +109,7 @@ def test_other_arguments_are_refused(L):
     for kw in (dict(start=None), dict(n=None), dict(batch=-1), dict(batch=65536), dict(max_new=-1)):
         assert append(L, s, **kw) == -1, kw
     assert append(L, s, batch=0) == 0 and append(L, s, max_new=0) == 0
-    for kw in (dict(lens=None), dict(out=None), dict(out=FAKE + 2), dict(batch=-1), dict(batch=65536), dict(n_q=-1), dict(splits=-1),
+    for kw in (dict(lens=None), dict(out=None), dict(out=FAR + 2), dict(batch=-1), dict(batch=65536), dict(n_q=-1), dict(splits=-1),
                dict(max_seq=-1), dict(max_seq=1025), dict(scale=float("nan")), dict(scale=float("inf")), dict(w_in=FAKE),
                dict(n_q=0, w_out=FAKE)):
         assert attend(L, s, **kw) == -1, kw
@@ -145,3 +145,30 @@ def test_an_eviction_into_the_cache_that_it_reads_is_refused(L):
 def test_shape_of_the_python_form():
     with pytest.raises(AssertionError):
         api.make_q8_shape(128, 8, 8, 1024, dtype=__import__("torch").float32)
+
+
+def test_an_append_to_one_cache_as_keys_and_values_is_refused(L):
+    s, one = shape(), lambda a, b=0: cache(codes=a * FAR + b, scales=a * FAR + b)
+    assert append(L, s, kc=one(1), vc=one(1)) == -1 and b"share" in L.nsn_last_error()
+    assert append(L, s, kc=one(1), vc=one(1, 1024)) == -1 and append(L, s, kc=one(1, 1024), vc=one(1)) == -1
+    paged = shape(page_size=64, n_pages=64)
+    t = lambda table: api.nsn_q8_cache(FAR, 2 * FAR, table)
+    assert append(L, paged, kc=t(FAKE), vc=t(FAKE)) == -1 and b"share" in L.nsn_last_error()
+
+
+def test_outputs_in_the_inputs_are_refused(L):
+    s = shape(n_q_heads=8, n_kv_heads=2)   # (rows: head stride 128, token stride 1024; a row is 2 * D bytes)
+    end = FAR + (3 * 1024 + 7 * 128 + s.head_dim) * 2
+    size = 4 * 8 * s.head_dim * 2
+    q = rows(FAR)
+    for out in (FAR, end - 16, FAR - size + 16):
+        assert attend(L, s, q=q, n_q=4, out=out) == -1 and b"out" in L.nsn_last_error(), out
+    back = rows(FAR, t=-1024)               # tokens in falling order
+    assert attend(L, s, q=back, n_q=4, out=FAR - 3 * 1024 * 2) == -1 and b"out" in L.nsn_last_error()
+    w = 2 * s.max_len * 4
+    for w_in in (FAKE, FAKE + 2 * w):
+        assert attend(L, s, q=q, out=FAR, w_in=w_in, w_out=FAKE + w, batch=2) == -1 and b"overlap" in L.nsn_last_error(), w_in
+    for new in (FAKE, FAKE + 4, FAKE - 4):
+        assert evict(L, s, new=new, batch=2) == -1 and b"new_lens" in L.nsn_last_error(), new
+    for w_out in (FAKE, FAKE + 64, FAKE - w + 64):
+        assert evict(L, s, w_out=w_out) == -1 and b"weights" in L.nsn_last_error(), w_out

@@ -396,7 +396,9 @@ int64_t nsn_q8_v_code_offset(const nsn_q8_shape* shape, int64_t t, int c);
 /*
  * Device bytes an operation needs, for sequences of up to max_seq_len tokens.
  *   NSN_OP_Q8_ATTENTION  n = n_q; n_splits as passed to nsn_q8_attention (0 = auto).  Fill the workspace with zeros
- *                        ONCE after allocating it; every call leaves it ready for the next one, of any size.
+ *                        ONCE after allocating it; every call leaves it ready for the next one, of any size.  A
+ *                        workspace of this size serves every call of n tokens over up to batch sequences of up to
+ *                        max_seq_len tokens.
  *   NSN_OP_Q8_EVICT      needs none: 0
  * It starts on a 16-byte boundary.  Calls that share a workspace must not overlap in time.  Returns 0 for an invalid shape or
  * size.

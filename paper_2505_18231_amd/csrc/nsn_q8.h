@@ -191,7 +191,7 @@ struct AttentionCall {
   void* workspace;
   hipStream_t stream;
 };
-size_t attention_workspace_bytes(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int n_splits, bool weights);
+size_t attention_workspace_bytes(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int n_splits);
 int attention_launch(const AttentionCall& c);
 
 struct EvictCall {

@@ -110,7 +110,7 @@ size_t nsn_q8_workspace_bytes(const nsn_q8_shape* shape, int op, int batch, int 
   if (check_shape(shape) != NSN_OK || batch <= 0 || batch > 65535 || n <= 0 || max_seq_len < 0 || max_seq_len > shape->max_len ||
       n_splits < 0)
     return 0;
-  if (op == NSN_OP_Q8_ATTENTION) return q8::attention_workspace_bytes(*shape, batch, n, max_seq_len, n_splits, true);
+  if (op == NSN_OP_Q8_ATTENTION) return q8::attention_workspace_bytes(*shape, batch, n, max_seq_len, n_splits);
   return 0;  // (an eviction needs none)
 }
 
@@ -173,7 +173,7 @@ int nsn_q8_attention(const nsn_q8_shape* shape, const nsn_rows* q, int n_q, cons
     set_error("q8_attention: n_q=%d times %d query heads per kv head is beyond 2^24", n_q, shape->n_q_heads / shape->n_kv_heads);
     return NSN_ERR_UNSUPPORTED;
   }
-  const size_t need = q8::attention_workspace_bytes(*shape, batch, n_q, max_seq_len, n_splits, weights_out != nullptr);
+  const size_t need = q8::attention_workspace_bytes(*shape, batch, n_q, max_seq_len, n_splits);
   if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0)) {
     set_error("q8_attention: a workspace of %zu bytes, 16-byte aligned, is needed", need);
     return NSN_ERR_WORKSPACE;

@@ -1115,6 +1115,9 @@ struct Plan {
   size_t lse2_at, partial_at, scores_at, bytes;
   int64_t score_stride;
 };
+// floats of a run's partial sums
+static size_t run_floats(bool chunk, int head_dim) { return 2 * (size_t)(chunk ? (head_dim / 2 + 4) * kWaves * 64 : 16 * (head_dim + 4)); }
+
 // ragged: sequences may have fewer queries than n_q
 static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int requested, bool weights, bool ragged) {
   Plan p;
@@ -1131,8 +1134,11 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   // blocks, but no more than a unit has: units one after the other cost their trips to memory one after the other
   const int64_t most = p.chunk ? 512 : kMaxCounters;
   // chunks of many units go one to a workgroup, as joining a cut tile's 128 rows costs about ten of its blocks: with 512 units of 128 to
-  // 160 blocks 355 us so and 372 us in equal runs; with ragged chunks of up to 512 units of very different lengths 114 us and 62 us
-  p.direct = requested <= 0 && (p.chunk ? units >= (ragged ? 1024 : 512) : units > most);
+  // 160 blocks 355 us so and 372 us in equal runs; with ragged chunks of up to 512 units of very different lengths 114 us and 62 us.
+  // So do units of few blocks, where joining is most of the time, unless so few of them that compute units are left idle
+  // (head_dim 128: 256 units of 5 blocks 20.0 us and 30.6, of 8 26 and 29; 384 of up to 15 blocks, equal 45 and 48, ragged 36 and 35;
+  // 128 of 8 23 and 18; ragged, up to 768 units of up to 16 blocks 40 and 43, of 32 77 and 67)
+  p.direct = requested <= 0 && (p.chunk ? (blocks <= 16 && blocks * (512 - units) <= 2048) || units >= (ragged ? 1024 : 512) : units > most);
   p.per = requested > 0 ? 1 : std::min(p.chunk && units < 128 ? 8 : 4, blocks);
   const int64_t runs = requested > 0 ? requested * units : p.chunk ? 512 : units <= 64 ? 256 : std::max<int64_t>(512, units);
   p.runs = p.direct ? (int)std::min<int64_t>(units, 0x7fffffff)
@@ -1141,7 +1147,7 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   // parts unequal, each with four tiles of rows at least; its partial sums come after the attention's and take their place
   p.weight_groups = (blocks + kWaves - 1) / kWaves * (int64_t)s.n_kv_heads * batch;
   p.weight_parts = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxCounters / p.weight_groups, rows / (4 * kWeightRows)));
-  size_t partials = p.direct ? 0 : (size_t)p.runs * 2 * (p.chunk ? (s.head_dim / 2 + 4) * kWaves * 64 : 16 * (s.head_dim + 4));
+  size_t partials = p.direct ? 0 : p.runs * run_floats(p.chunk, s.head_dim);
   p.scores = weights && rows <= 16;
   if (weights && p.weight_parts > 1) partials = std::max(partials, (size_t)p.weight_groups * p.weight_parts * kWeightTokens);
   p.score_stride = (int64_t)blocks * kBlock;
@@ -1152,8 +1158,17 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   return p;
 }
 
-size_t attention_workspace_bytes(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int n_splits, bool weights) {
-  return std::max(plan_of(s, batch, n_q, max_seq_len, n_splits, weights, false).bytes, plan_of(s, batch, n_q, max_seq_len, n_splits, weights, true).bytes);
+// For calls of up to these sizes, with or without weights: as many runs of either kind as any plan of them has
+size_t attention_workspace_bytes(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, int n_splits) {
+  const Plan p = plan_of(s, batch, n_q, max_seq_len, n_splits, true, false);
+  const int64_t rows = (int64_t)n_q * (s.n_q_heads / s.n_kv_heads), heads = (int64_t)s.n_kv_heads * batch, blocks = p.score_stride / kBlock;
+  auto most = [&](bool chunk, int64_t limit) {
+    const int64_t units = (rows + (chunk ? 32 * kWaves : 16) - 1) / (chunk ? 32 * kWaves : 16) * heads;
+    return (size_t)std::min(limit, units * blocks) * run_floats(chunk, s.head_dim);
+  };
+  size_t partials = std::max(most(false, kMaxCounters), p.chunk ? most(true, 512) : 0);
+  if (rows >= 8 * kWeightRows) partials = std::max(partials, (size_t)kMaxCounters * kWeightTokens);
+  return p.partial_at + up16(partials * sizeof(float)) + (p.bytes - p.scores_at);
 }
 
 int attention_launch(const AttentionCall& c) {

@@ -307,9 +307,9 @@ __global__ __launch_bounds__(T) void select_kernel(int hkv, int max_len, const f
 // ---- eviction: the kept tokens move -----------------------------------------------------------------------
 // One workgroup per 64-token block of the destination and head, K and V together: the block's 64 former indices and scales, one
 // per lane, give the new scale and each token's ratio; then the rows' cells are all asked for, rounded again where the
-// ratio is not 1, and written.  Bound by memory: each kept byte is read and written once; the way from the indices over the
-// pages and scales to the first row is four trips, which only other workgroups of the compute unit cover (64 heads of 4096 kept
-// tokens, 142 MB: 37 us with a block to a workgroup, 52 us with four).
+// ratio is not 1, and written.  Bound by memory: each kept byte is read and written once, and of values, whose tokens share 16-byte
+// cells, the neighbours of a kept token come along (64 heads of 4096 of up to 16384 tokens: 37 us, 142 MB, 178 with the
+// neighbours; four blocks to a workgroup measured the same).
 constexpr int kMoveThreads = 256;
 
 // four codes of a live token under a scale that is 1 / r times theirs, r <= 1

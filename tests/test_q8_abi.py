@@ -172,3 +172,16 @@ def test_outputs_in_the_inputs_are_refused(L):
         assert evict(L, s, new=new, batch=2) == -1 and b"new_lens" in L.nsn_last_error(), new
     for w_out in (FAKE, FAKE + 64, FAKE - w + 64):
         assert evict(L, s, w_out=w_out) == -1 and b"weights" in L.nsn_last_error(), w_out
+
+
+def test_a_workspace_serves_fewer_and_shorter_sequences(L):
+    rng = np.random.default_rng(3)
+    for _ in range(300):
+        d, kv, ratio = int(rng.choice([64, 128])), int(rng.choice([1, 2, 8, 12, 32])), int(rng.choice([1, 4, 7]))
+        s = api.make_q8_shape(d, kv * ratio, kv, 1 << 20)
+        n, batch, length = int(np.exp(rng.uniform(0, 8))), int(np.exp(rng.uniform(0, 5))), int(np.exp(rng.uniform(0, 12)))
+        size = lambda b, m: api.nsn_q8_workspace_bytes(s, api.NSN_OP_Q8_ATTENTION, b, n, m)  # noqa: E731
+        most = size(batch, length)
+        for _ in range(8):
+            b, m = int(rng.integers(1, batch + 1)), int(rng.integers(0, length + 1))
+            assert 0 < size(b, m) <= most, (d, kv, ratio, n, batch, length, b, m)

@@ -220,18 +220,20 @@ struct Fetched {
 // Then sum p v = sref / 2^kLift * (what o holds), sum p = l / 2^kLift with l += (sum p') * (sref / sv).  The output is divided by the sum
 // of the weights as they were rounded (lr), so that a token that holds nearly all of the weight comes out exact; lse goes by l.
 constexpr int kLazy = 4, kSpan = 4, kLift = 6;
+constexpr float kMost = 60000.f;
 
-// top: the row's largest score of the block; ratio = sref / sv, lift = kLift + log2(sv / sref) for the block
+// moves a row's maximum to m_new
 template <int N, typename V>
-__device__ __forceinline__ void running(float top, float sv, float& m, float& l, float& lr, float& sref, V (&o)[N], float& ratio, float& lift) {
-  if (__any(top > m + kLazy)) {  // (each row by its own scores: its result does not hang on its neighbours)
-    const float m_new = top > m + kLazy ? top : m;
-    const float alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
-    m = m_new;
-    l *= alpha, lr *= alpha;
+__device__ __forceinline__ void move_maximum(float m_new, float& m, float& l, float& lr, V (&o)[N]) {
+  const float alpha = m == m_new ? 1.f : fast_exp2(m - m_new);
+  m = m_new;
+  l *= alpha, lr *= alpha;
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[i] *= alpha;
-  }
+  for (int i = 0; i < N; ++i) o[i] *= alpha;
+}
+// ratio = sref / sv, lift = kLift + log2(sv / sref) for a block
+template <int N, typename V>
+__device__ __forceinline__ void follow_scale(float sv, float& sref, V (&o)[N], float& ratio, float& lift) {
   ratio = 1.f, lift = kLift;
   if (sv > 0.f) {
     // (a jump of more than 2^60 downwards would take the sums out of range: weights that small count as they underflow)
@@ -486,8 +488,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void rows_kernel(Args a) {
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[j][e]);
     top = fmaxf(top, xor_lane<16>(top));
     top = fmaxf(top, xor_lane<32>(top)) * f;
+    if (__any(top > m + kLazy)) move_maximum<kCh>(top > m + kLazy ? top : m, m, l, lr, o);  // (each row by its own scores)
     float ratio, lift;
-    running<kCh>(top, x.sv, m, l, lr, sref, o, ratio, lift);
+    follow_scale<kCh>(x.sv, sref, o, ratio, lift);
     const float base = m - lift;
     float sum = 0.f, rounded = 0.f;
     half8v p[2];
@@ -683,6 +686,11 @@ struct ChunkTile {
   _Float16 v[D][kValRow];  // row 16 i + n: channel (D / 16) n + i; place 16 st + 8 hh + j: token 16 st + 8 (j / 4) + 4 hh + j % 4
 };
 
+// operands of a tile that are asked for ahead of their products: LDS answers in about three products' time
+constexpr int kAhead = 6;
+// products and reads of LDS stay in the order written (left to itself the compiler puts each read before its product, to wait for it)
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0x002 | 0x004 | 0x200); }
+
 template <int D, int CODE, bool BF>
 __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
   constexpr int kCh = D / 16, kTok = 256 / D, kCellsOf4 = 4 / kTok, kKeyCells = D / 64;
@@ -780,69 +788,89 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     if (there && t0 < vis_max) {
       const ChunkTile<D>& tl = sm[buf];
       float16v s[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8v*>(&tl.k[32 * j + n][16 * ks + 8 * hh]), q[ks], s[j], 0, 0, 0);
-      // (six operands asked for ahead of the first product, then one per product: LDS answers in about three products' time)
-      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-      for (int i = 0; i < D / 8 - 6; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
       const float f = factor * sk;
       const bool masked = t0 + kBlock > vis_min;
-      if (masked) {
+      auto scores = [&] {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) s[j][e] = kMasked;
-      }
-      float top = s[0][0];
+          for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
+        half8v x[kAhead];
+        auto read = [&](int i) { x[i % kAhead] = *reinterpret_cast<const half8v*>(&tl.k[32 * (i & 1) + n][16 * (i / 2) + 8 * hh]); };
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[j][e]);
-      top = fmaxf(top, xor_lane<32>(top)) * f;
+        for (int i = 0; i < D / 8; ++i) {
+          in_order();
+          s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], q[i / 2], s[i & 1], 0, 0, 0);
+          if (i + kAhead < D / 8) read(i + kAhead);
+        }
+      };
+      auto hide = [&](float with) {  // the tokens that a row does not see, a bit each (compares would take the scalar registers)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int left = vis - t0 - 4 * hh - 32 * j;  // of these 32
+          const int seen = left >= 32 ? -1 : (1 << max(left, 0)) - 1;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int own = __builtin_amdgcn_sbfe(seen, 8 * (e / 4) + e % 4, 1);  // all ones, or 0
+            s[j][e] = __uint_as_float((__float_as_uint(s[j][e]) & own) | (__float_as_uint(with) & ~own));
+          }
+        }
+      };
+      float sum[2];
+      auto weights = [&](float base) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[j][e] = fast_exp2(fmaf(s[j][e], f, -base));
+        if (masked) hide(0.f);
+        sum[0] = sum[1] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) sum[0] += s[j][e], sum[1] += s[j][e + 1];
+      };
+      scores();
       float ratio, lift;
-      running<D / 32>(top, sv, m, l, lr, sref, o, ratio, lift);
-      const float base = m - lift;
-      float sum[2] = {0.f, 0.f}, rounded[2] = {0.f, 0.f};
+      follow_scale<D / 32>(sv, sref, o, ratio, lift);
+      weights(m - lift);
+      // The weights under the maximum as it was will do unless they come near the end of fp16; only then (the first tile, a
+      // rise of more than 2^5) are the scores formed again for their maximum.
+      const float most = fmaxf(sum[0] + sum[1], xor_lane<32>(sum[0] + sum[1]));
+      if (__any(!(most < kMost))) {
+        scores();
+        if (masked) hide(kMasked);
+        float top = s[0][0];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[j][e]);
+        top = fmaxf(top, xor_lane<32>(top)) * f;
+        move_maximum<D / 32>(most < kMost ? m : fmaxf(m, top), m, l, lr, o);  // (each row by its own weights: its result does not hang on its neighbours)
+        weights(m - lift);
+      }
+      float rounded[2] = {0.f, 0.f};
       half8v p[4];
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[j][e] = fast_exp2(fmaf(s[j][e], f, -base));
-      if (masked) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (t0 + 32 * j + 8 * (e / 4) + 4 * hh + e % 4 >= vis) s[j][e] = 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          sum[0] += s[j][e], sum[1] += s[j][e + 1];
           const half2v u = __builtin_convertvector((float2v{s[j][e], s[j][e + 1]}), half2v);
           rounded[j] = add_rounded(u, rounded[j]);
           p[2 * j + e / 8][e % 8] = u[0], p[2 * j + e / 8][e % 8 + 1] = u[1];
         }
       add_weights(sum[0] + sum[1], rounded[0] + rounded[1], ratio, l, lr);
+      half8v x[kAhead];
+      auto read = [&](int i) { x[i % kAhead] = *reinterpret_cast<const half8v*>(&tl.v[i % (D / 32) * 32 + n][16 * (i / (D / 32)) + 8 * hh]); };
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+      for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-          o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8v*>(&tl.v[32 * i + n][16 * st + 8 * hh]), p[st], o[i], 0, 0, 0);
+      for (int i = 0; i < D / 8; ++i) {
+        in_order();
+        o[i % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], p[i / (D / 32)], o[i % (D / 32)], 0, 0, 0);
+        if (i + kAhead < D / 8) read(i + kAhead);
+      }
     }
     if (blk + 1 < blk1 && next_there) stage(sm[buf ^ 1]);
   }

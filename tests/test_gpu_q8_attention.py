@@ -203,6 +203,25 @@ def test_large_and_small_scores_and_values(gpu_api, io, n_q):
         run(gpu_api, rng, dev, 4, lens, n_q, weights=True, spread=0.0)
 
 
+@pytest.mark.parametrize("n_q,hkv", [(1, 2), (40, 64)])
+@pytest.mark.parametrize("code", [INT8, E4M3])
+def test_scales_that_jump_from_block_to_block(gpu_api, code, n_q, hkv):
+    """Blocks whose keys, then whose values, are many powers of two larger or smaller than those of the block before: the tokens that
+    hold all the weight may be those with the smallest values."""
+    import torch
+    lens = [700, 330]
+    rng, dev = make(gpu_api, 19, code, 128, "bf16", hkv, 1, lens, 704)
+    powers = {"k": [0, 1, 4, 0, 6, 2, 7, 3, 0, 8, 5], "v": [0, 20, -100, 0, -100, -60, -100, 20, -30, -100, 0]}
+    for kind, e in powers.items():
+        by = np.exp2(np.array(e, dtype=np.float64))
+        for b in range(2):
+            for h in range(hkv):
+                dev.ref[kind][b][h].s *= by[:len(dev.ref[kind][b][h].s)].astype(dev.ref[kind][b][h].s.dtype)
+        dev.cache[kind].scales *= torch.from_numpy(by).float().cuda()
+    run(gpu_api, rng, dev, 1, lens, n_q, spread=0.3)
+    run(gpu_api, rng, dev, 1, lens, n_q, weights=True, causal=True, spread=0.3)
+
+
 def test_a_nan_stays_in_its_row(gpu_api):
     import torch
     rng, dev = make(gpu_api, 21, E4M3, 128, "fp16", 2, 2, [300], 320)

@@ -716,7 +716,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
   const int last = min(rw + 31, n_rows - 1);
   const int vis_min = rw < n_rows ? visible(a, pr, rw / a.g.ratio) : 0, vis_max = rw < n_rows ? visible(a, pr, last / a.g.ratio) : 0;
   const int vis_all = visible(a, pr, min(r0 + 32 * kWaves - 1, n_rows - 1) / a.g.ratio);
-  const int blk0 = cur.first(), blk1 = min((vis_all + kBlock - 1) / kBlock, cur.last()), first_run = cur.first_run(), live = cur.runs();
+  const int blk0 = cur.first(), blk1 = min((vis_all + kBlock - 1) / kBlock, cur.last());
 
   half8v q[D / 16];
   const float factor = load_query_rows<D, BF>(a, b, h, r, pr.nq, q);
@@ -881,6 +881,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     if (blk + 1 < blk1 && next_there) stage(sm[buf ^ 1]);
   }
   l += xor_lane<32>(l), lr += xor_lane<32>(lr);
+  const int first_run = cur.first_run(), live = cur.runs();  // (here: scalar registers are short in the loop)
   // o[i][e]: row 32 i + 8 (e / 4) + 4 hh + e % 4 of the transposed values; the channels of cell c are its rows 16 x + c
   float M = l == 0.f ? -INFINITY : m - kLift, unit_of_o = sref;
   [&] {
@@ -888,36 +889,59 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     // the sums as they lie in the threads, two to a store; joined in the order of the runs
     constexpr int kPairs = D / 4, kThreads = kWaves * 64;
     auto partial_of = [&](int k) { return a.partial + (((int64_t)(first_run + k) * 2 + (k == 0)) * (kPairs + 2) * kThreads + tid) * 2; };
-    float* P = partial_of(cur.run - first_run);
-    if (r < n_rows) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) store_agent(P + (8 * i + e / 2) * kThreads * 2, o[i][e] * sref, o[i][e + 1] * sref);
-      store_agent(P + kPairs * kThreads * 2, M, l);
-      store_agent(P + (kPairs + 1) * kThreads * 2, lr, 0.f);
-    }
-    if (!arrives_last(a, 0, first_run, live, arrived)) return;
-    M = -INFINITY, l = lr = 0.f, unit_of_o = 1.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    if (r < n_rows)
-      for (int k = 0; k < live; ++k) {
-        const float* ps = partial_of(k);
-        const float2v ml = load_agent(ps + kPairs * kThreads * 2), rd = load_agent(ps + (kPairs + 1) * kThreads * 2);
-        float2v x[kPairs];
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) x[i] = load_agent(ps + i * kThreads * 2);
-        const float m2 = fmaxf(M, ml[0]), turn = part_factor(M, m2), f = part_factor(ml[0], m2);
-        M = m2;
-        l = fmaf(f, ml[1], l * turn), lr = fmaf(f, rd[0], lr * turn);
+    for (int i = 0; i < D / 32; ++i) o[i] *= sref;
+    unit_of_o = 1.f;
+    // all of them where they are few; of more than 16, eight at a time, and then those sums (two tiles of eight heads over 30000 tokens:
+    // 100 us in one go, 70 us so)
+    constexpr int kGroup = 8;
+    const bool two = live > 2 * kGroup;
+    int mine = cur.run - first_run, from = two ? mine / kGroup * kGroup : 0, n_parts = two ? min(kGroup, live - from) : live, step = 1;
+    int kind = two ? (from == 0 ? 1 : 2) : 0;
+    while (true) {
+      float* P = partial_of(mine);
+      if (r < n_rows) {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[i][e] = fmaf(f, x[8 * i + e / 2][e & 1], o[i][e] * turn);
+          for (int e = 0; e < 16; e += 2) store_agent(P + (8 * i + e / 2) * kThreads * 2, o[i][e], o[i][e + 1]);
+        store_agent(P + kPairs * kThreads * 2, M, l);
+        store_agent(P + (kPairs + 1) * kThreads * 2, lr, 0.f);
       }
+      if (!arrives_last(a, kind, first_run + from, n_parts, arrived)) return;
+      // in the order of the runs, whoever joins them; its own sums it still holds
+      float16v total[D / 32];
+      float m_all = -INFINITY, l_all = 0.f, lr_all = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) total[i][e] = 0.f;
+      if (r < n_rows)
+        for (int k = from; k < from + n_parts * step; k += step) {
+          float2v ml = {M, l}, rd = {lr, 0.f}, x[kPairs];
+          if (k == mine) {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) x[i] = float2v{o[i / 8][i % 8 * 2], o[i / 8][i % 8 * 2 + 1]};
+          } else {
+            const float* ps = partial_of(k);
+            ml = load_agent(ps + kPairs * kThreads * 2), rd = load_agent(ps + (kPairs + 1) * kThreads * 2);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) x[i] = load_agent(ps + i * kThreads * 2);
+          }
+          const float m2 = fmaxf(m_all, ml[0]), turn = part_factor(m_all, m2), f = part_factor(ml[0], m2);
+          m_all = m2;
+          l_all = fmaf(f, ml[1], l_all * turn), lr_all = fmaf(f, rd[0], lr_all * turn);
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) total[i][e] = fmaf(f, x[8 * i + e / 2][e & 1], total[i][e] * turn);
+        }
+      M = m_all, l = l_all, lr = lr_all;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) o[i] = total[i];
+      if (!two || step > 1) break;
+      mine = from, from = 0, n_parts = (live + kGroup - 1) / kGroup, step = kGroup, kind = 0;
+    }
   }
   if (r >= n_rows) return;
   const int64_t place = ((int64_t)b * a.n_q + r / a.g.ratio) * a.g.hq + h * a.g.ratio + r % a.g.ratio;

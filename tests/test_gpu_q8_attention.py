@@ -158,6 +158,14 @@ def test_a_long_chunk_of_few_heads(gpu_api, code, D):
     run(gpu_api, rng, dev, 1, lens, 2048, nq=[129])
 
 
+@pytest.mark.parametrize("code,D,n_q,lens", [(INT8, 64, 260, [107000]), (E4M3, 128, 150, [60000, 30000, 40])])
+def test_a_few_tiles_over_very_many_tokens(gpu_api, code, D, n_q, lens):
+    """A tile of rows that reaches into far more than sixteen runs: its sums are joined in two steps."""
+    rng, dev = make(gpu_api, 83, code, D, "bf16", 1, 1, lens, 107008 if D == 64 else 60032)
+    run(gpu_api, rng, dev, 1, lens, n_q, causal=True, spread=0.3)
+    run(gpu_api, rng, dev, 1, lens, n_q, splits=23, spread=0.3)
+
+
 @pytest.mark.parametrize("code,D,io", [(INT8, 128, "fp16"), (E4M3, 64, "bf16")])
 @pytest.mark.parametrize("n_q,ratio", [(1, 1), (1, 5), (3, 7)])
 def test_units_that_reach_into_many_runs(gpu_api, code, D, io, n_q, ratio):

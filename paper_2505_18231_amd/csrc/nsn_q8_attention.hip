@@ -696,7 +696,8 @@ constexpr int kAhead = 6;
 // products and reads of LDS stay in the order written (left to itself the compiler puts each read before its product, to wait for it)
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0x002 | 0x004 | 0x200); }
 
-template <int D, int CODE, bool BF>
+// FEW: few tiles, which may reach into many runs each; apart, as that code costs the other calls 4 % (chunk of 2048 over 10240 tokens)
+template <int D, int CODE, bool BF, bool FEW>
 __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
   constexpr int kCh = D / 16, kTok = 256 / D, kCellsOf4 = 4 / kTok, kKeyCells = D / 64;
   __shared__ ChunkTile<D> sm[2];
@@ -895,7 +896,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void chunk_kernel(Args a) {
     // all of them where they are few; of more than 16, eight at a time, and then those sums (two tiles of eight heads over 30000 tokens:
     // 100 us in one go, 70 us so)
     constexpr int kGroup = 8;
-    const bool two = live > 2 * kGroup;
+    const bool two = FEW && live > 2 * kGroup;
     int mine = cur.run - first_run, from = two ? mine / kGroup * kGroup : 0, n_parts = two ? min(kGroup, live - from) : live, step = 1;
     int kind = two ? (from == 0 ? 1 : 2) : 0;
     while (true) {
@@ -1258,8 +1259,10 @@ int attention_launch(const AttentionCall& c) {
       set_error("q8_attention: batch * n_q * n_q_heads * max_seq_len is too large for one launch");
       return NSN_ERR_UNSUPPORTED;
     }
-    if (plan.chunk)
-      chunk_kernel<D, CODE, BF><<<plan.runs, kWaves * 64, 0, c.stream>>>(a);
+    if (plan.chunk && units <= 32)
+      chunk_kernel<D, CODE, BF, true><<<plan.runs, kWaves * 64, 0, c.stream>>>(a);
+    else if (plan.chunk)
+      chunk_kernel<D, CODE, BF, false><<<plan.runs, kWaves * 64, 0, c.stream>>>(a);
     else
       rows_kernel<D, CODE, BF><<<plan.runs, kWaves * 64, 0, c.stream>>>(a);
     if (hipGetLastError() != hipSuccess) return NSN_ERR_HIP;

@@ -1193,7 +1193,7 @@ static Plan plan_of(const nsn_q8_shape& s, int batch, int n_q, int max_seq_len, 
   // blocks, but no more than a unit has: units one after the other cost their trips to memory one after the other
   const int64_t most = p.chunk ? 512 : kMaxCounters;
   // chunks of many units go one to a workgroup, as joining a cut tile's 128 rows costs about ten of its blocks: with 512 units of 128 to
-  // 160 blocks 355 us so and 372 us in equal runs; with ragged chunks of up to 512 units of very different lengths 114 us and 62 us.
+  // 160 blocks 355 us so and 372 us in equal runs (now 342 so); with ragged chunks of up to 512 units of very different lengths 114 us and 62 us.
   // So do units of few blocks, where joining is most of the time, unless so few of them that compute units are left idle
   // (head_dim 128: 256 units of 5 blocks 20.0 us and 30.6, of 8 26 and 29; 384 of up to 15 blocks, equal 45 and 48, ragged 36 and 35;
   // 128 of 8 23 and 18; ragged, up to 768 units of up to 16 blocks 40 and 43, of 32 77 and 67)
